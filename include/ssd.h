@@ -214,6 +214,72 @@ int ssd_verify_from_probs(const float* dev_pt, const float* dev_pd, const int32_
 int ssd_warp_probs(const float* dev_logits, int rows, int V, const ssd_sample_config* cfg,
                    float* dev_probs, void* stream);
 
+/* ---- the paged cache's steps alone -----------------------------------------------------------------------
+ * For engines that run a decoder of their own over pages: what a step of a ragged batch does to the cache, with any number of new rows per
+ * sequence (decoding, verification and prompts in one batch) and, where the batch speaks behind one prefix - a voice prompt, an
+ * instruction -, with that prefix kept and read once.  The calls keep no state and synchronise nothing; all of them can be captured, and a replay reads
+ * lengths, tables and rows as they then are.  Arrays of one call must not overlap except where it is said.
+ *   Sequence s has dev_len[s] cached positions; its new rows stand at positions dev_len[s] ..  Position p is token p % block_tokens of
+ * block dev_table[s * table_cap + p / block_tokens].  The first dev_shared[s] (>= 0; a null dev_shared: none) entries are not its own: it neither
+ * takes nor gives them back, and with new rows it has at least that many whole blocks of cached positions.
+ *   Conditions that only the device can see are bits of a status word. */
+#define SSD_STATUS_POOL  1    /* fewer free blocks than the step takes */
+#define SSD_STATUS_TABLE 2    /* a sequence needs more than table_cap blocks */
+#define SSD_STATUS_ROWS  4    /* more new rows than max_rows */
+#define SSD_STATUS_BATCH 8    /* a length, row count, block count or position that cannot be */
+#define SSD_STATUS_PAGE 16    /* a block id or slot outside the pool, or a position beyond the table */
+
+/* One layer's pages, in the layout of ssd_kv's pool: keys [n_blocks][n_kv_heads][block_tokens][head_dim] after the rotary embedding, values
+ * [n_blocks][n_kv_heads][head_dim][block_tokens], 16-byte aligned.  head_dim in {32,64,128}, block_tokens a power of two from 16 to 1024
+ * (else SSD_ENOSUP); n_blocks * block_tokens < 2^31.  Positions that were never written may hold anything, NaN included. */
+typedef struct {
+  void*   dev_keys;
+  void*   dev_values;
+  int32_t n_blocks, n_kv_heads, block_tokens, head_dim;
+  int32_t dtype;        /* SSD_DTYPE_* of the pages, and of the queries, keys, values and outputs of the calls below */
+} ssd_pages;
+
+/* Blocks and slots of a step.  Sequence s needs ceil((len + rows) / block_tokens) - shared blocks of its own and holds dev_owned[s] of them, entries
+ * shared .. shared + owned - 1 of its table; a request that is over has rows 0 and a len of no more than its shared blocks.  The bookkeeping is that of
+ * ssd_kv_state: first the sequences, ascending, push back what they no longer need, highest index first, then, ascending, pop what they
+ * lack.  dev_free_stack has n_blocks entries, the first dev_n_free[0] are free, the last of these is popped next.  Written: the popped ids
+ * into dev_table (entries behind a sequence's blocks are left as they were), what was pushed into dev_free_stack, the new counts to dev_owned_out
+ * [n_seqs] and dev_n_free_out [1] (which may be the input arrays), dev_row_start [n_seqs + 1] (row r of the step is one of s for row_start[s] <= r
+ * < row_start[s + 1]) and of each row its sequence, position and slot, block * block_tokens + token, [max_rows] each; -1 for rows behind the
+ * last.  dev_status[0] is set: 0, or SSD_STATUS_* bits, and then nothing has moved: tables, stack and counts are as before, row_start all 0 and
+ * rows -1, so that the calls below do nothing.  n_seqs <= 4096 (else SSD_ENOSUP).  dev_len and dev_rows are not changed. */
+int ssd_block_tables(int n_seqs, int block_tokens, int n_blocks, int table_cap, int max_rows, const int32_t* dev_len, const int32_t* dev_rows,
+                     const int32_t* dev_shared, const int32_t* dev_owned, const int32_t* dev_n_free, int32_t* dev_table, int32_t* dev_free_stack,
+                     int32_t* dev_owned_out, int32_t* dev_n_free_out, int32_t* dev_row_start, int32_t* dev_row_seq, int32_t* dev_row_pos,
+                     int32_t* dev_row_slot, int32_t* dev_status, void* stream);
+
+/* Rotary embedding and append (step a4 of a verification): for each of n_rows rows (0 allowed) the pairs (i, i + head_dim/2) of its n_q_heads query
+ * heads and of its key heads are turned by the angles of dev_row_pos[r] - cosines and sines dev_rope [rope_positions][head_dim/2][2] fp32; null:
+ * nothing is turned -, in fp32 and rounded once; queries go to dev_q_out (which may be dev_q), keys and values to slot dev_row_slot[r].  Rows are heads of
+ * head_dim behind each other, `stride` elements from row to row (columns of one QKV product as well), beginning at multiples of 16 bytes.
+ * n_q_heads 0: keys and values alone.  A row with a negative position is left out, one with a negative slot is not appended; a slot outside the pool
+ * or a position outside dev_rope is left out and ORed to dev_status[0] (may be null).  Slots >= 0 are distinct: of two rows with one slot either
+ * may win, element by element. */
+int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads, const void* dev_q, size_t q_stride, const void* dev_k, size_t k_stride,
+                    const void* dev_v, size_t v_stride, const float* dev_rope, int rope_positions, const int32_t* dev_row_pos,
+                    const int32_t* dev_row_slot, void* dev_q_out, size_t q_out_stride, int32_t* dev_status, void* stream);
+
+/* Attention of rows 0 .. dev_row_start[n_seqs]-1 (n_rows bounds them; rows behind are not written): softmax of scale * q . k over the positions up to the
+ * row's own, times the values.  Query head h reads key/value head h / (n_q_heads / n_kv_heads).  The first shared_blocks blocks (0: none)
+ * are a prefix, block ids dev_shared_table [shared_blocks], that every sequence with at least its positions cached has in front - with
+ * dev_shared given, those of dev_shared[s] >= shared_blocks; others read all positions through their own table.  The prefix is read once for all
+ * rows, not through the sequences' tables.  max_len: about the largest len + rows; it decides how the keys are cut, not what is read, and a
+ * wrong one costs time only.  The result of a row depends on how its call is cut, by the rounding of sums in another order, and the same call gives the same
+ * bits.  Sums and softmax are fp32; with bf16 pages the weights are rounded to bf16 for their product with the values.
+ *   A position whose block is not in the pool or not in the table is left out, and SSD_STATUS_PAGE ORed to dev_status[0] (may be null); a row that has
+ * no position left gets zeros.  dev_ws: ssd_paged_attention_workspace_bytes(), which may be 0, and (size_t)-1 for arguments that the call refuses; calls
+ * that may overlap need workspaces of their own.  n_rows * n_q_heads <= 2^26, n_seqs <= 65536, table_cap * block_tokens <= 2^30. */
+size_t ssd_paged_attention_workspace_bytes(const ssd_pages* pages, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks);
+int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float scale, int n_seqs, int n_rows, int max_len, const int32_t* dev_len,
+                        const int32_t* dev_row_start, const int32_t* dev_table, int table_cap, int shared_blocks, const int32_t* dev_shared_table,
+                        const int32_t* dev_shared, const void* dev_q, size_t q_stride, void* dev_out, size_t out_stride, void* dev_ws,
+                        size_t ws_bytes, int32_t* dev_status, void* stream);
+
 /* ---- introspection (synchronises `stream`) -------------------------------------------------------------
  * Bookkeeping contract: a forward that writes R rows makes each sequence (ascending) own
  * ceil((len+R)/block_tokens) blocks, popping the free stack; a commit or rollback to new_len pushes back the

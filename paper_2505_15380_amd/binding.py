@@ -13,6 +13,7 @@ EXPORTED_SYMBOLS = [
     "ssd_kv_free_stack", "ssd_profile_begin", "ssd_profile_end", "ssd_kv_last_forward_path", "ssd_trace_barriers", "ssd_strerror", "ssd_last_error",
     "ssd_verify_noalloc", "ssd_kv_clear_error", "ssd_kv_test_hook", "ssd_cycle_create", "ssd_cycle_launch", "ssd_cycle_captures", "ssd_cycle_destroy",
     "ssd_gemm_plan", "ssd_gemm_blocks", "ssd_prompt_gemm_plan", "ssd_attention_plan", "ssd_resident_fits",
+    "ssd_block_tables", "ssd_rope_append", "ssd_paged_attention_workspace_bytes", "ssd_paged_attention",
 ]
 
 
@@ -31,6 +32,11 @@ class ModelConfig(C.Structure):
 class SampleConfig(C.Structure):
     _fields_ = [("beta", C.c_float), ("temperature", C.c_float), ("top_k", C.c_int32), ("greedy", C.c_int32),
                 ("seed", C.c_uint64)]
+
+
+class _Pages(C.Structure):
+    _fields_ = [("dev_keys", C.c_void_p), ("dev_values", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_blocks", "n_kv_heads", "block_tokens", "head_dim", "dtype")]
 
 
 def sample_config(beta=0.0, temperature=1.0, top_k=0, greedy=False, seed=0):
@@ -90,6 +96,11 @@ def load_library():
         "ssd_gemm_blocks": (i32, [i32, i32, i32, i32, i32, C.POINTER(C.c_int), i32]),
         "ssd_attention_plan": (i32, [i32, i32, i32, i32, i32, i32, i32, C.POINTER(C.c_int)]),
         "ssd_resident_fits": (i32, [C.POINTER(C.c_int), i32, i32, i32, i32]),
+        "ssd_block_tables": (i32, [i32] * 5 + [i32p] * 14 + [vp]),
+        "ssd_rope_append": (i32, [C.POINTER(_Pages), i32, i32, vp, sz, vp, sz, vp, sz, f32p, i32, i32p, i32p, vp, sz, i32p, vp]),
+        "ssd_paged_attention_workspace_bytes": (sz, [C.POINTER(_Pages), i32, i32, i32, i32, i32]),
+        "ssd_paged_attention": (i32, [C.POINTER(_Pages), i32, C.c_float, i32, i32, i32, i32p, i32p, i32p, i32, i32, i32p, i32p, vp, sz, vp, sz,
+                                      vp, sz, i32p, vp]),
         "ssd_strerror": (C.c_char_p, [i32]),
         "ssd_last_error": (C.c_char_p, []),
     }
@@ -207,6 +218,11 @@ class KVCache:
         if getattr(self, "handle", None) and _LIB is not None:
             _LIB.ssd_kv_destroy(self.handle)
             self.handle = None
+
+    def pages(self, layer):
+        """The pages of one layer, for the calls that take Pages."""
+        k = self.pool[layer, 0]
+        return Pages(k, self.pool[layer, 1].view(self.n_blocks, k.shape[1], k.shape[3], k.shape[2]))
 
     def state(self, seq):
         lib = load_library()
@@ -363,6 +379,114 @@ def ssd_warp_probs(logits, cfg):
     probs = torch.empty_like(logits)
     _check(load_library().ssd_warp_probs(_ptr(logits), rows, V, C.byref(cfg), _ptr(probs), _stream()))
     return probs
+
+
+STATUS_POOL, STATUS_TABLE, STATUS_ROWS, STATUS_BATCH, STATUS_PAGE = 1, 2, 4, 8, 16
+
+
+def _need(ok, what):
+    if not ok:
+        raise SSDError(-1, what)
+
+
+def _ints(dev, **arrays):
+    """int32 arrays (None is skipped) that lie in one piece on device `dev`, which has to be the current one: the calls go to its current stream."""
+    _need(dev.type == "cuda" and dev.index == torch.cuda.current_device(), f"tensors are on {dev}, which is not the current device")
+    for name, (t, n) in arrays.items():
+        _need(t is None or (t.dtype == torch.int32 and t.device == dev and t.is_contiguous() and t.numel() >= n),
+              f"{name}: at least {n} int32 in one piece on {dev}")
+
+
+class Pages:
+    """One layer's keys [n_blocks, n_kv_heads, block_tokens, head_dim] and values [n_blocks, n_kv_heads, head_dim, block_tokens]."""
+
+    def __init__(self, keys, values):
+        nb, nkv, bt, hd = keys.shape
+        _need(keys.dtype == values.dtype and keys.dtype in (torch.bfloat16, torch.float32), "pages are bf16 or fp32")
+        _need(values.shape == (nb, nkv, hd, bt) and values.device == keys.device, "values are [n_blocks, n_kv_heads, head_dim, block_tokens] on the keys' device")
+        _need(keys.is_contiguous() and values.is_contiguous(), "pages lie in one piece")
+        self.keys, self.values = keys, values
+        self.c = _Pages(keys.data_ptr(), values.data_ptr(), nb, nkv, bt, hd, 1 if keys.dtype == torch.bfloat16 else 0)
+        self.ref = C.byref(self.c)
+
+    def rows(self, name, t, heads):
+        """Row stride of [rows, heads, head_dim] whose rows are in one piece each."""
+        _need(t.dtype == self.keys.dtype and t.device == self.keys.device, f"{name} has the pages' type and device")
+        _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == self.c.head_dim, f"{name} is [rows, {heads}, {self.c.head_dim}]")
+        st = t.stride()
+        _need(st[2] == 1 and (heads == 1 or st[1] == self.c.head_dim), f"the heads of a row of {name} lie behind each other")
+        return st[0] if t.shape[0] > 1 else heads * self.c.head_dim
+
+
+def ssd_block_tables(lens, rows, block_tokens, table, owned, free_stack, n_free, max_rows, shared=None, out=None):
+    """Blocks and slots of a step.  lens, rows, owned[, shared] [n_seqs], table [n_seqs, cap], free_stack [n_blocks], n_free [1]: int32 device
+    tensors; table and free_stack are written.  Returns dict(owned, n_free, row_start [n_seqs + 1], row_seq, row_pos, row_slot [max_rows],
+    status [1]); `out`: the tensors to write (owned and n_free may be the inputs)."""
+    B, cap = table.shape
+    if out is None:
+        e = lambda n: torch.empty(n, dtype=torch.int32, device=table.device)      # noqa: E731
+        out = dict(owned=e(B), n_free=e(1), row_start=e(B + 1), row_seq=e(max_rows), row_pos=e(max_rows), row_slot=e(max_rows), status=e(1))
+    _ints(table.device, lens=(lens, B), rows=(rows, B), table=(table, B * cap), owned=(owned, B), free_stack=(free_stack, 1), n_free=(n_free, 1), shared=(shared, B),
+          owned_out=(out["owned"], B), n_free_out=(out["n_free"], 1), row_start=(out["row_start"], B + 1), row_seq=(out["row_seq"], max_rows),
+          row_pos=(out["row_pos"], max_rows), row_slot=(out["row_slot"], max_rows), status=(out["status"], 1))
+    _check(load_library().ssd_block_tables(B, block_tokens, free_stack.numel(), cap, max_rows, _ptr(lens), _ptr(rows), _ptr(shared), _ptr(owned), _ptr(n_free), _ptr(table),
+                                           _ptr(free_stack), _ptr(out["owned"]), _ptr(out["n_free"]), _ptr(out["row_start"]), _ptr(out["row_seq"]),
+                                           _ptr(out["row_pos"]), _ptr(out["row_slot"]), _ptr(out["status"]), _stream()))
+    return out
+
+
+def ssd_rope_append(pages, row_pos, row_slot, k, v, q=None, rope=None, q_out=None, status=None):
+    """Rotary embedding of q and k and the append of k and v.  k, v [rows, n_kv_heads, head_dim], q [rows, n_q_heads, head_dim] or None (columns of one
+    QKV product will do), rope [positions, head_dim / 2, 2] fp32 or None, row_pos, row_slot [rows] int32.  Returns q_out."""
+    n, nkv = k.shape[0], pages.c.n_kv_heads
+    ks, vs = pages.rows("k", k, nkv), pages.rows("v", v, nkv)
+    nq, qs, os_ = 0, 0, 0
+    _need(v.shape[0] == n, "k and v have the same rows")
+    if q is not None:
+        nq = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _need(q.shape[0] == n and q_out.shape == q.shape, "q and q_out have the rows of k")
+        qs, os_ = pages.rows("q", q, nq), pages.rows("q_out", q_out, nq)
+    _ints(k.device, row_pos=(row_pos, n), row_slot=(row_slot, n), status=(status, 1))
+    _need(rope is None or (rope.dtype == torch.float32 and rope.device == k.device and rope.is_contiguous() and rope.dim() == 3 and rope.shape[1:] == (pages.c.head_dim // 2, 2)),
+          "rope is [positions, head_dim / 2, 2] fp32 in one piece")
+    _check(load_library().ssd_rope_append(pages.ref, n, nq, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(rope), 0 if rope is None else rope.shape[0], _ptr(row_pos),
+                                          _ptr(row_slot), _ptr(q_out), os_, _ptr(status), _stream()))
+    return q_out
+
+
+def ssd_paged_attention(pages, q, lens, row_start, table, scale=None, shared_table=None, shared=None, max_len=None, out=None, ws=None, status=None):
+    """Attention of q [n_rows, n_q_heads, head_dim] over the pages of its sequences: lens [n_seqs], row_start [n_seqs + 1], table [n_seqs, cap], and
+    shared_table [shared_blocks], shared [n_seqs] of a common prefix, int32.  scale: 1 / sqrt(head_dim) unless given.  max_len: about the largest len + rows (what the table
+    holds unless given).  ws: a uint8 device tensor of paged_attention_workspace() bytes, unless it is to be allocated here.  Returns out."""
+    n, nq = q.shape[0], q.shape[1]
+    B, cap = table.shape
+    c = pages.c
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _need(out.shape == q.shape, "out has the shape of q")
+    qs, os_ = pages.rows("q", q, nq), pages.rows("out", out, nq)
+    sb = 0 if shared_table is None else shared_table.numel()
+    _ints(q.device, lens=(lens, B), row_start=(row_start, B + 1), table=(table, B * cap), shared_table=(shared_table, sb), shared=(shared, B), status=(status, 1))
+    if max_len is None:
+        max_len = cap * c.block_tokens
+    if ws is None:
+        need = paged_attention_workspace(pages, nq, B, n, max_len, sb)
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _need(ws is None or (ws.dtype == torch.uint8 and ws.device == q.device and ws.is_contiguous()), "ws is a uint8 tensor in one piece on the device of q")
+    _check(load_library().ssd_paged_attention(pages.ref, nq, c.head_dim ** -0.5 if scale is None else float(scale), B, n, max_len, _ptr(lens), _ptr(row_start), _ptr(table), cap,
+                                              sb, _ptr(shared_table) if sb else None, _ptr(shared), _ptr(q), qs, _ptr(out), os_, _ptr(ws),
+                                              0 if ws is None else ws.numel(), _ptr(status), _stream()))
+    return out
+
+
+def paged_attention_workspace(pages, n_q_heads, n_seqs, n_rows, max_len, shared_blocks=0):
+    """Bytes of ssd_paged_attention's workspace for such a call."""
+    need = load_library().ssd_paged_attention_workspace_bytes(pages.ref, n_q_heads, n_seqs, n_rows, max_len, shared_blocks)
+    if need == C.c_size_t(-1).value:
+        raise SSDError(-1, load_library().ssd_last_error().decode())
+    return need
 
 
 PROFILE_KINDS = {"qkv": 0, "attention": 1, "o": 2, "gate_up": 3, "down": 4, "head": 5, "persistent": 6}

@@ -21,6 +21,7 @@
 
 #include "attention.h"
 #include "common.h"
+#include "errors.h"
 #include "gemm.h"
 #include "gemm_tile.h"
 #include "persistent.h"
@@ -33,7 +34,7 @@ using namespace ssd;
 
 // ------------------------------------------------------------------------------------------------ errors
 static thread_local std::string g_err;
-static int fail(int code, const char* fmt, ...) {
+int ssd::fail(int code, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -42,12 +43,6 @@ static int fail(int code, const char* fmt, ...) {
   g_err = buf;
   return code;
 }
-#define HIP_TRY(expr)                                                                      \
-  do {                                                                                     \
-    hipError_t e_ = (expr);                                                                \
-    if (e_ != hipSuccess) return fail(SSD_EHIP, "%s: %s", #expr, hipGetErrorString(e_));   \
-  } while (0)
-#define LAUNCH_CHECK() HIP_TRY(hipGetLastError())
 
 extern "C" const char* ssd_strerror(int code) {
   switch (code) {
