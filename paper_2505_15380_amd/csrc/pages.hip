@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "errors.h"
 #include "pages.h"
@@ -15,6 +16,7 @@ using namespace ssd;
 
 static_assert(ST_POOL == SSD_STATUS_POOL && ST_TABLE == SSD_STATUS_TABLE && ST_ROWS == SSD_STATUS_ROWS && ST_BAD == SSD_STATUS_BATCH && ST_PAGE == SSD_STATUS_PAGE, "");
 
+static inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 static int log2_of(int v) {
   int s = 0;
   while ((1 << s) < v) ++s;
@@ -96,22 +98,27 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
 // ------------------------------------------------------------------------------------------------ attention
 // How a call is cut.  From sizes that the caller gives alone, so that the workspace's size is known without a device.
 struct AttnCut {
+  int sh_rows, own_rows;                                   // packed query rows of a workgroup: 16 (k_paged_attention), 128 or 256 (k_paged_tiles)
   int P, P_sh, sh_chunks, own_chunks, sh_slots, own_slots;
 };
-static AttnCut cut_attention(int nkv, int group, int n_seqs, int n_rows, int max_len, int shared_positions) {
-  constexpr int WANT = 1024;                               // workgroups: four to a compute unit
+static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, int n_rows, int max_len, int shared_positions) {
   AttnCut c;
-  c.own_slots = n_rows * group / 16 + n_seqs;
-  c.sh_slots = shared_positions ? (n_rows * group + 15) / 16 : 0;
-  auto parts = [&](int slots, int keys) {
-    const int chunks = std::max(1, (keys + PA_CHUNK - 1) / PA_CHUNK);
-    const int want = std::max(1, WANT / std::max(1, slots * nkv));
-    return std::max(1, std::min({want, (chunks + PA_WAVES - 1) / PA_WAVES, 64}));
+  const int packed = n_rows * group;
+  auto tile = [&](int rows) { return dtype != SSD_DTYPE_BF16 || rows < 48 ? 16 : hd == 128 || rows < 1024 ? 128 : 256; };
+  auto parts = [&](int tile, int slots, int keys) {
+    const int chunks = std::max(1, cdiv(keys, PA_CHUNK));
+    const int want = std::max(1, (tile > 16 ? 512 : 1024) / std::max(1, slots * nkv));
+    return std::max(1, std::min({want, cdiv(chunks, 4), 64}));
   };
-  const int own = std::max(1, max_len - shared_positions), own_parts = parts(n_seqs, own);
-  c.own_chunks = ((own + PA_CHUNK - 1) / PA_CHUNK + own_parts - 1) / own_parts;
-  c.P_sh = shared_positions ? parts(c.sh_slots, shared_positions) : 0;
-  c.sh_chunks = c.P_sh ? ((shared_positions + PA_CHUNK - 1) / PA_CHUNK + c.P_sh - 1) / c.P_sh : 0;
+  c.sh_rows = tile(packed);
+  c.own_rows = tile(packed / n_seqs);
+  c.own_slots = packed / c.own_rows + n_seqs;
+  c.sh_slots = shared_positions ? cdiv(packed, c.sh_rows) : 0;
+  const int own = std::max(1, max_len - shared_positions), own_parts = parts(c.own_rows, std::max(n_seqs, packed / c.own_rows), own);
+  c.own_chunks = cdiv(cdiv(own, PA_CHUNK), own_parts);
+  c.P_sh = shared_positions ? parts(c.sh_rows, c.sh_slots, shared_positions) : 0;
+  c.sh_chunks = c.P_sh ? cdiv(cdiv(shared_positions, PA_CHUNK), c.P_sh) : 0;
+  if (c.P_sh) c.P_sh = cdiv(cdiv(shared_positions, PA_CHUNK), c.sh_chunks);
   c.P = c.P_sh + own_parts;
   return c;
 }
@@ -128,15 +135,32 @@ static size_t attention_ws(const AttnCut& c, int n_rows, int nq, int hd) { retur
 extern "C" size_t ssd_paged_attention_workspace_bytes(const ssd_pages* pages, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks) {
   Pages p;
   if (check_attention(pages, p, n_q_heads, n_seqs, n_rows, max_len, shared_blocks)) return (size_t)-1;
-  return attention_ws(cut_attention(p.nkv, n_q_heads / p.nkv, n_seqs, n_rows, max_len, shared_blocks * p.bt), n_rows, n_q_heads, p.hd);
+  return attention_ws(cut_attention(pages->dtype, p.hd, p.nkv, n_q_heads / p.nkv, n_seqs, n_rows, max_len, shared_blocks * p.bt), n_rows, n_q_heads, p.hd);
 }
 
+// `rows`: packed query rows of a workgroup; `shared`, `own`: which sources of keys this launch takes.
 template <typename DT, int HD>
-static int launch_paged_attention(const PagedAttnArgs& a, hipStream_t st) {
+static int launch_paged_source(PagedAttnArgs a, int rows, bool shared, bool own, hipStream_t st) {
+  if (!shared) a.sh_slots = 0;
+  if (!own) a.own_slots = 0;
   const long long wgs = ((long long)a.sh_slots * a.P_sh + (long long)a.own_slots * (a.P - a.P_sh)) * a.p.nkv;
+  if (wgs == 0) return SSD_OK;
   if (wgs > 0x7FFFFFFFll) return fail(SSD_ENOSUP, "too many workgroups");
-  hipLaunchKernelGGL((k_paged_attention<DT, HD>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
+  if constexpr (std::is_same<DT, BF16>::value) {
+    if (rows == 128) hipLaunchKernelGGL((k_paged_tiles<HD, 1>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
+    if constexpr (HD < 128)
+      if (rows == 256) hipLaunchKernelGGL((k_paged_tiles<HD, 2>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
+  }
+  if (rows == 16) hipLaunchKernelGGL((k_paged_attention<DT, HD>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
   LAUNCH_CHECK();
+  return SSD_OK;
+}
+template <typename DT, int HD>
+static int launch_paged_attention(const PagedAttnArgs& a, const AttnCut& c, hipStream_t st) {
+  const bool one = c.sh_rows == c.own_rows;
+  if (int rc = launch_paged_source<DT, HD>(a, c.own_rows, one, true, st)) return rc;
+  if (!one)
+    if (int rc = launch_paged_source<DT, HD>(a, c.sh_rows, true, false, st)) return rc;
   if (a.P > 1) {
     hipLaunchKernelGGL((k_paged_attention_merge<DT, HD>), dim3((unsigned)((a.n_rows * a.nq + 3) / 4)), dim3(BLOCK), 0, st, a);
     LAUNCH_CHECK();
@@ -156,7 +180,7 @@ extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float 
   if (int rc = check_rows("q", dev_q, q_stride, n_q_heads, a.p, pages->dtype)) return rc;
   if (int rc = check_rows("out", dev_out, out_stride, n_q_heads, a.p, pages->dtype)) return rc;
   if (n_rows == 0) return SSD_OK;
-  const AttnCut c = cut_attention(a.p.nkv, n_q_heads / a.p.nkv, n_seqs, n_rows, max_len, shared_blocks * a.p.bt);
+  const AttnCut c = cut_attention(pages->dtype, a.p.hd, a.p.nkv, n_q_heads / a.p.nkv, n_seqs, n_rows, max_len, shared_blocks * a.p.bt);
   const size_t need = attention_ws(c, n_rows, n_q_heads, a.p.hd);
   if (need && (!dev_ws || ((uintptr_t)dev_ws & 15))) return fail(SSD_EINVAL, "workspace is null or not 16-byte aligned");
   if (ws_bytes < need) return fail(SSD_ENOMEM, "attention workspace: need %zu bytes, got %zu", need, ws_bytes);
@@ -170,8 +194,8 @@ extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float 
   hipStream_t st = (hipStream_t)stream;
   const bool b16 = pages->dtype == SSD_DTYPE_BF16;
   switch (a.p.hd) {
-    case 32: return b16 ? launch_paged_attention<BF16, 32>(a, st) : launch_paged_attention<F32, 32>(a, st);
-    case 64: return b16 ? launch_paged_attention<BF16, 64>(a, st) : launch_paged_attention<F32, 64>(a, st);
-    default: return b16 ? launch_paged_attention<BF16, 128>(a, st) : launch_paged_attention<F32, 128>(a, st);
+    case 32: return b16 ? launch_paged_attention<BF16, 32>(a, c, st) : launch_paged_attention<F32, 32>(a, c, st);
+    case 64: return b16 ? launch_paged_attention<BF16, 64>(a, c, st) : launch_paged_attention<F32, 64>(a, c, st);
+    default: return b16 ? launch_paged_attention<BF16, 128>(a, c, st) : launch_paged_attention<F32, 128>(a, c, st);
   }
 }
