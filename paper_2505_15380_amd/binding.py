@@ -384,38 +384,50 @@ def ssd_warp_probs(logits, cfg):
 STATUS_POOL, STATUS_TABLE, STATUS_ROWS, STATUS_BATCH, STATUS_PAGE = 1, 2, 4, 8, 16
 
 
-def _need(ok, what):
-    if not ok:
-        raise SSDError(-1, what)
+_I32 = torch.int32
+_PAGE_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
-def _ints(dev, **arrays):
-    """int32 arrays (None is skipped) that lie in one piece on device `dev`, which has to be the current one: the calls go to its current stream."""
-    _need(dev.type == "cuda" and dev.index == torch.cuda.current_device(), f"tensors are on {dev}, which is not the current device")
-    for name, (t, n) in arrays.items():
-        _need(t is None or (t.dtype == torch.int32 and t.device == dev and t.is_contiguous() and t.numel() >= n),
-              f"{name}: at least {n} int32 in one piece on {dev}")
+def _device_is_current(t):
+    """Index of the tensor's device, which has to be the current one: the calls go to its current stream."""
+    dev = t.get_device()
+    if dev < 0 or dev != (torch.cuda.current_device() if _current_device is None or not torch.cuda.is_initialized() else _current_device()):
+        raise SSDError(-1, f"tensors are on {t.device}, which is not the current device")
+    return dev
+
+
+# (A step calls these three for every layer, and the host's part of a small one is most of it: what can be wrong is asked in one expression a tensor, and put into words
+# only when it is.)
+def _int_array(name, t, dev, n):
+    """At least n int32 in one piece on the device."""
+    if t.dtype is not _I32 or t.numel() < n or t.get_device() != dev or not t.is_contiguous():
+        raise SSDError(-1, f"{name}: at least {n} int32 in one piece on the device of the pages")
+    return t.data_ptr()
 
 
 class Pages:
     """One layer's keys [n_blocks, n_kv_heads, block_tokens, head_dim] and values [n_blocks, n_kv_heads, head_dim, block_tokens]."""
 
+    __slots__ = ("keys", "values", "c", "ref", "dtype", "head_dim", "n_kv_heads", "block_tokens", "dev")
+
     def __init__(self, keys, values):
         nb, nkv, bt, hd = keys.shape
-        _need(keys.dtype == values.dtype and keys.dtype in (torch.bfloat16, torch.float32), "pages are bf16 or fp32")
-        _need(values.shape == (nb, nkv, hd, bt) and values.device == keys.device, "values are [n_blocks, n_kv_heads, head_dim, block_tokens] on the keys' device")
-        _need(keys.is_contiguous() and values.is_contiguous(), "pages lie in one piece")
+        self.dtype, self.dev = keys.dtype, keys.get_device()
+        if self.dtype not in _PAGE_DTYPES or values.dtype is not self.dtype or values.shape != (nb, nkv, hd, bt) or values.get_device() != self.dev or \
+                not keys.is_contiguous() or not values.is_contiguous():
+            raise SSDError(-1, "pages are keys [n_blocks, n_kv_heads, block_tokens, head_dim] and values [n_blocks, n_kv_heads, head_dim, block_tokens], bf16 or fp32, "
+                               "each in one piece and both on one device")
         self.keys, self.values = keys, values
-        self.c = _Pages(keys.data_ptr(), values.data_ptr(), nb, nkv, bt, hd, 1 if keys.dtype == torch.bfloat16 else 0)
+        self.n_kv_heads, self.block_tokens, self.head_dim = nkv, bt, hd
+        self.c = _Pages(keys.data_ptr(), values.data_ptr(), nb, nkv, bt, hd, _PAGE_DTYPES[self.dtype])
         self.ref = C.byref(self.c)
 
     def rows(self, name, t, heads):
         """Row stride of [rows, heads, head_dim] whose rows are in one piece each."""
-        _need(t.dtype == self.keys.dtype and t.device == self.keys.device, f"{name} has the pages' type and device")
-        _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == self.c.head_dim, f"{name} is [rows, {heads}, {self.c.head_dim}]")
-        st = t.stride()
-        _need(st[2] == 1 and (heads == 1 or st[1] == self.c.head_dim), f"the heads of a row of {name} lie behind each other")
-        return st[0] if t.shape[0] > 1 else heads * self.c.head_dim
+        sh, st, hd = t.shape, t.stride(), self.head_dim
+        if t.dtype is not self.dtype or t.get_device() != self.dev or len(sh) != 3 or sh[1] != heads or sh[2] != hd or st[2] != 1 or (st[1] != hd and heads != 1):
+            raise SSDError(-1, f"{name} is [rows, {heads}, {hd}] of the pages' type and device, the heads of a row behind each other")
+        return st[0] if sh[0] > 1 else heads * hd
 
 
 def ssd_block_tables(lens, rows, block_tokens, table, owned, free_stack, n_free, max_rows, shared=None, out=None):
@@ -423,36 +435,39 @@ def ssd_block_tables(lens, rows, block_tokens, table, owned, free_stack, n_free,
     tensors; table and free_stack are written.  Returns dict(owned, n_free, row_start [n_seqs + 1], row_seq, row_pos, row_slot [max_rows],
     status [1]); `out`: the tensors to write (owned and n_free may be the inputs)."""
     B, cap = table.shape
+    dev, a = _device_is_current(table), _int_array
     if out is None:
         e = lambda n: torch.empty(n, dtype=torch.int32, device=table.device)      # noqa: E731
         out = dict(owned=e(B), n_free=e(1), row_start=e(B + 1), row_seq=e(max_rows), row_pos=e(max_rows), row_slot=e(max_rows), status=e(1))
-    _ints(table.device, lens=(lens, B), rows=(rows, B), table=(table, B * cap), owned=(owned, B), free_stack=(free_stack, 1), n_free=(n_free, 1), shared=(shared, B),
-          owned_out=(out["owned"], B), n_free_out=(out["n_free"], 1), row_start=(out["row_start"], B + 1), row_seq=(out["row_seq"], max_rows),
-          row_pos=(out["row_pos"], max_rows), row_slot=(out["row_slot"], max_rows), status=(out["status"], 1))
-    _check(load_library().ssd_block_tables(B, block_tokens, free_stack.numel(), cap, max_rows, _ptr(lens), _ptr(rows), _ptr(shared), _ptr(owned), _ptr(n_free), _ptr(table),
-                                           _ptr(free_stack), _ptr(out["owned"]), _ptr(out["n_free"]), _ptr(out["row_start"]), _ptr(out["row_seq"]),
-                                           _ptr(out["row_pos"]), _ptr(out["row_slot"]), _ptr(out["status"]), _stream()))
+    _check(load_library().ssd_block_tables(
+        B, block_tokens, free_stack.numel(), cap, max_rows, a("lens", lens, dev, B), a("rows", rows, dev, B), None if shared is None else a("shared", shared, dev, B),
+        a("owned", owned, dev, B), a("n_free", n_free, dev, 1), a("table", table, dev, 1), a("free_stack", free_stack, dev, 1), a("out['owned']", out["owned"], dev, B),
+        a("out['n_free']", out["n_free"], dev, 1), a("out['row_start']", out["row_start"], dev, B + 1), a("out['row_seq']", out["row_seq"], dev, max_rows),
+        a("out['row_pos']", out["row_pos"], dev, max_rows), a("out['row_slot']", out["row_slot"], dev, max_rows), a("out['status']", out["status"], dev, 1), _stream()))
     return out
 
 
 def ssd_rope_append(pages, row_pos, row_slot, k, v, q=None, rope=None, q_out=None, status=None):
     """Rotary embedding of q and k and the append of k and v.  k, v [rows, n_kv_heads, head_dim], q [rows, n_q_heads, head_dim] or None (columns of one
     QKV product will do), rope [positions, head_dim / 2, 2] fp32 or None, row_pos, row_slot [rows] int32.  Returns q_out."""
-    n, nkv = k.shape[0], pages.c.n_kv_heads
+    n, nkv, dev = len(k), pages.n_kv_heads, _device_is_current(pages.keys)
     ks, vs = pages.rows("k", k, nkv), pages.rows("v", v, nkv)
-    nq, qs, os_ = 0, 0, 0
-    _need(v.shape[0] == n, "k and v have the same rows")
+    nq = qs = os_ = 0
+    if len(v) != n:
+        raise SSDError(-1, "k and v have the same rows")
     if q is not None:
         nq = q.shape[1]
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _need(q.shape[0] == n and q_out.shape == q.shape, "q and q_out have the rows of k")
         qs, os_ = pages.rows("q", q, nq), pages.rows("q_out", q_out, nq)
-    _ints(k.device, row_pos=(row_pos, n), row_slot=(row_slot, n), status=(status, 1))
-    _need(rope is None or (rope.dtype == torch.float32 and rope.device == k.device and rope.is_contiguous() and rope.dim() == 3 and rope.shape[1:] == (pages.c.head_dim // 2, 2)),
-          "rope is [positions, head_dim / 2, 2] fp32 in one piece")
-    _check(load_library().ssd_rope_append(pages.ref, n, nq, _ptr(q), qs, _ptr(k), ks, _ptr(v), vs, _ptr(rope), 0 if rope is None else rope.shape[0], _ptr(row_pos),
-                                          _ptr(row_slot), _ptr(q_out), os_, _ptr(status), _stream()))
+        if len(q) != n or len(q_out) != n:
+            raise SSDError(-1, "q and q_out have the rows of k")
+    if rope is not None and (rope.dtype is not torch.float32 or rope.get_device() != dev or not rope.is_contiguous() or rope.shape[1:] != (pages.head_dim // 2, 2)):
+        raise SSDError(-1, "rope is [positions, head_dim / 2, 2] fp32 in one piece on the device of the pages")
+    _check(load_library().ssd_rope_append(
+        pages.ref, n, nq, None if q is None else q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, None if rope is None else rope.data_ptr(), 0 if rope is None else len(rope),
+        _int_array("row_pos", row_pos, dev, n), _int_array("row_slot", row_slot, dev, n), None if q is None else q_out.data_ptr(), os_,
+        None if status is None else _int_array("status", status, dev, 1), _stream()))
     return q_out
 
 
@@ -460,24 +475,26 @@ def ssd_paged_attention(pages, q, lens, row_start, table, scale=None, shared_tab
     """Attention of q [n_rows, n_q_heads, head_dim] over the pages of its sequences: lens [n_seqs], row_start [n_seqs + 1], table [n_seqs, cap], and
     shared_table [shared_blocks], shared [n_seqs] of a common prefix, int32.  scale: 1 / sqrt(head_dim) unless given.  max_len: about the largest len + rows (what the table
     holds unless given).  ws: a uint8 device tensor of paged_attention_workspace() bytes, unless it is to be allocated here.  Returns out."""
-    n, nq = q.shape[0], q.shape[1]
+    n, nq, hd = q.shape
     B, cap = table.shape
-    c = pages.c
+    dev, a = _device_is_current(pages.keys), _int_array
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _need(out.shape == q.shape, "out has the shape of q")
+    elif len(out) != n:
+        raise SSDError(-1, "out has the rows of q")
     qs, os_ = pages.rows("q", q, nq), pages.rows("out", out, nq)
     sb = 0 if shared_table is None else shared_table.numel()
-    _ints(q.device, lens=(lens, B), row_start=(row_start, B + 1), table=(table, B * cap), shared_table=(shared_table, sb), shared=(shared, B), status=(status, 1))
     if max_len is None:
-        max_len = cap * c.block_tokens
+        max_len = cap * pages.block_tokens
     if ws is None:
         need = paged_attention_workspace(pages, nq, B, n, max_len, sb)
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    _need(ws is None or (ws.dtype == torch.uint8 and ws.device == q.device and ws.is_contiguous()), "ws is a uint8 tensor in one piece on the device of q")
-    _check(load_library().ssd_paged_attention(pages.ref, nq, c.head_dim ** -0.5 if scale is None else float(scale), B, n, max_len, _ptr(lens), _ptr(row_start), _ptr(table), cap,
-                                              sb, _ptr(shared_table) if sb else None, _ptr(shared), _ptr(q), qs, _ptr(out), os_, _ptr(ws),
-                                              0 if ws is None else ws.numel(), _ptr(status), _stream()))
+    elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
+        raise SSDError(-1, "ws is a uint8 tensor in one piece on the device of the pages")
+    _check(load_library().ssd_paged_attention(
+        pages.ref, nq, hd ** -0.5 if scale is None else scale, B, n, max_len, a("lens", lens, dev, B), a("row_start", row_start, dev, B + 1), a("table", table, dev, 1), cap,
+        sb, a("shared_table", shared_table, dev, sb) if sb else None, None if shared is None else a("shared", shared, dev, B), q.data_ptr(), qs, out.data_ptr(), os_,
+        None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), None if status is None else a("status", status, dev, 1), _stream()))
     return out
 
 

@@ -16,9 +16,24 @@ struct Pages {
 // Bits of a status word (the public header's SSD_STATUS_*).
 constexpr int ST_POOL = 1, ST_TABLE = 2, ST_ROWS = 4, ST_BAD = 8, ST_PAGE = 16;
 
+// Largest s in [0, n) with base(s) <= x, for base ascending from base(0) <= x; all lanes of the wave call it.
+template <typename F>
+__device__ __forceinline__ int wave_search(int n, int x, F base) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, step = 1;
+  while (step * 64 < n) step *= 64;
+  for (;; step /= 64) {
+    const int s = lo + lane * step;
+    const unsigned long long m = __ballot(s < n && base(s) <= x);
+    lo += (63 - __builtin_clzll(m | 1ull)) * step;
+    if (step == 1) return lo;
+  }
+}
+
 // ---------------------------------------------------------------------------------------------- block tables
 constexpr int BT_MAX_SEQS = 4096;      // sequences of a call: three prefix sums of them stand in LDS
 constexpr int BT_THREADS = 1024;
+constexpr int BT_ROWS_HERE = 4096;     // rows that k_block_tables looks up itself; more go to a launch of their own
 
 struct BlockTableArgs {
   const int32_t *len, *rows, *owned, *shared, *n_free;
@@ -76,6 +91,10 @@ __device__ __forceinline__ int owner_of(const int* ends, int B, int i) {
   return lo;
 }
 
+__device__ __forceinline__ int slot_of(const BlockTableArgs& a, int seq, int pos) {
+  return (a.table[(size_t)seq * a.cap + (pos >> a.bt_shift)] << a.bt_shift) + (pos & ((1 << a.bt_shift) - 1));
+}
+
 // The serial walk that the bookkeeping is defined by - sequences in ascending order give back what they no longer need, highest index first, then
 // in ascending order take what they lack - as prefix sums: they say where on the stack each sequence's blocks go and come from.  One workgroup:
 // what it puts on the stack it takes from there again behind a barrier.
@@ -113,7 +132,8 @@ __global__ void __launch_bounds__(BT_THREADS) k_block_tables(BlockTableArgs a) {
   }
   if (bad) {
     for (int s = tid; s < B; s += BT_THREADS) { a.owned_out[s] = a.owned[s]; a.row_start[s + 1] = 0; }
-    for (int r = tid; r < a.max_rows; r += BT_THREADS) a.row_seq[r] = a.row_pos[r] = a.row_slot[r] = -1;
+    if (a.max_rows <= BT_ROWS_HERE)
+      for (int r = tid; r < a.max_rows; r += BT_THREADS) a.row_seq[r] = a.row_pos[r] = a.row_slot[r] = -1;
     return;
   }
   __syncthreads();
@@ -131,22 +151,46 @@ __global__ void __launch_bounds__(BT_THREADS) k_block_tables(BlockTableArgs a) {
     a.table[(size_t)s * a.cap + (a.shared ? a.shared[s] : 0) + a.owned[s] + (i - first)] = a.stack[F + G - 1 - i];
   }
   __syncthreads();
+  if (a.max_rows <= BT_ROWS_HERE)
 #pragma unroll 1
-  for (int r = tid; r < a.max_rows; r += BT_THREADS) {
-    int seq = -1, pos = -1, slot = -1;
-    if (r < R) {
-      seq = owner_of(rowed, B, r);
-      pos = a.len[seq] + r - (seq ? rowed[seq - 1] : 0);
-      slot = (a.table[(size_t)seq * a.cap + (pos >> a.bt_shift)] << a.bt_shift) + (pos & ((1 << a.bt_shift) - 1));
+    for (int r = tid; r < a.max_rows; r += BT_THREADS) {
+      int seq = -1, pos = -1, slot = -1;
+      if (r < R) {
+        seq = owner_of(rowed, B, r);
+        pos = a.len[seq] + r - (seq ? rowed[seq - 1] : 0);
+        slot = slot_of(a, seq, pos);
+      }
+      a.row_seq[r] = seq; a.row_pos[r] = pos; a.row_slot[r] = slot;
     }
-    a.row_seq[r] = seq; a.row_pos[r] = pos; a.row_slot[r] = slot;
-  }
   __syncthreads();                                         // (owned_out may be owned)
   for (int s = tid; s < B; s += BT_THREADS) {
     const int g = gave[s] - (s ? gave[s - 1] : 0), t = took[s] - (s ? took[s - 1] : 0);
     a.owned_out[s] = a.owned[s] - g + t;
     a.row_start[s + 1] = rowed[s];
   }
+}
+
+// Sequence, position and slot of every row of a step that has many, behind k_block_tables: one thread per row, whose sequence is searched for first among the
+// workgroup's, which stand side by side.
+__global__ void __launch_bounds__(BLOCK) k_block_table_rows(BlockTableArgs a) {
+  const int r = blockIdx.x * BLOCK + threadIdx.x;
+  const int all = a.row_start[a.B];                        // (0 if the step could not be)
+  int seq = -1, pos = -1, slot = -1;
+  const int w = blockIdx.x * BLOCK + (threadIdx.x & ~63);  // the wave's first row
+  if (w < all) {                                           // (the whole wave)
+    int lo = wave_search(a.B, w, [&](int s) { return a.row_start[s]; });
+    int hi = wave_search(a.B, min(w + 63, all - 1), [&](int s) { return a.row_start[s]; });
+    if (r < all) {
+      while (lo < hi) {                                    // the last of those that begin at or before the row
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.row_start[mid] <= r) lo = mid; else hi = mid - 1;
+      }
+      seq = lo;
+      pos = a.len[seq] + r - a.row_start[seq];
+      slot = slot_of(a, seq, pos);
+    }
+  }
+  if (r < a.max_rows) { a.row_seq[r] = seq; a.row_pos[r] = pos; a.row_slot[r] = slot; }
 }
 
 // ---------------------------------------------------------------------------------------------- rotary embedding and append
@@ -161,45 +205,135 @@ struct RopeAppendArgs {
   int n_rows, nq, positions;
 };
 
-// One thread per pair of a row's head.
+constexpr int RA_HEADS = 4;            // heads of a thread
+constexpr int RA_WINDOW = 64;          // rows of a workgroup that puts values
+
+// 16 bytes of a row as floats, and back, rounded once.
 template <typename DT>
-__global__ void __launch_bounds__(BLOCK) k_rope_append(RopeAppendArgs a) {
+struct Unit;
+template <>
+struct Unit<BF16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(const bf16_t* p, float (&x)[8]) {
+    const u32x4 v = *(const u32x4*)p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(v[e] << 16); x[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u); }
+  }
+  static __device__ __forceinline__ void put(bf16_t* p, const float (&x)[8]) {
+    *(u32x4*)p = u32x4{f2_to_bf16x2(x[0], x[1]), f2_to_bf16x2(x[2], x[3]), f2_to_bf16x2(x[4], x[5]), f2_to_bf16x2(x[6], x[7])};
+  }
+};
+template <>
+struct Unit<F32> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void get(const float* p, float (&x)[4]) { *(f32x4*)x = *(const f32x4*)p; }
+  static __device__ __forceinline__ void put(float* p, const float (&x)[4]) { *(f32x4*)p = *(const f32x4*)x; }
+};
+
+// The first `v_wgs` workgroups put values, the others turn queries and keys.
+//   Turning: a thread has 16 bytes of a row's first half of dims, the 16 of the second half that they are paired with, and their angles, for four
+// heads in turn.
+//   Values lie [dim][token], and a row brings one token of every dim: a workgroup takes 64 rows of a head through LDS and writes, for each dim, the
+// eight tokens of an aligned piece at once (16 bytes; fp32 32) where eight rows behind each other fill one, the piece of a row being the business
+// of the workgroup that has its first row; what fills no piece goes element by element.
+template <typename DT>
+__global__ void __launch_bounds__(BLOCK) k_rope_append(RopeAppendArgs a, int v_wgs) {
   typedef typename DT::T T;
-  const int hd = a.p.hd, half = hd >> 1, heads = a.nq + 2 * a.p.nkv;
-  const size_t i = (size_t)blockIdx.x * BLOCK + threadIdx.x;
-  const int row = (int)(i / ((size_t)heads * half));
+  constexpr int N = Unit<DT>::N, PIECE = 8, ROWS = RA_WINDOW + PIECE - 1;
+  __shared__ __align__(16) T vals[ROWS][128 + 16 / sizeof(T)];
+  __shared__ int slots[PIECE - 1 + ROWS];                  // of rows r0 - 7 ..
+  __shared__ int kind[ROWS];                               // 1: first row of a full piece, 2: by itself
+  const int hd = a.p.hd, tid = threadIdx.x;
+  if ((int)blockIdx.x < v_wgs) {
+    const int head = blockIdx.x % a.p.nkv, r0 = blockIdx.x / a.p.nkv * RA_WINDOW;
+    if (tid < PIECE - 1 + ROWS) {
+      const int r = r0 - (PIECE - 1) + tid;
+      int s = -1;
+      if (r >= 0 && r < a.n_rows) {
+        s = a.row_slot[r];
+        const bool out = s >= 0 && (s >> a.p.bt_shift) >= a.p.n_blocks;
+        if (out && a.status) atomicOr(a.status, ST_PAGE);
+        if (out || a.row_pos[r] < 0 || (a.rope && a.row_pos[r] >= a.positions)) s = -1;
+      }
+      slots[tid] = s;
+    }
+    const int per = hd / N;
+    for (int i = tid; i < ROWS * per; i += BLOCK) {
+      const int r = i / per, u = i - r * per;
+      if (r0 + r < a.n_rows) *(u32x4*)&vals[r][u * N] = *(const u32x4*)((const T*)a.v + (size_t)(r0 + r) * a.v_stride + head * hd + u * N);
+    }
+    __syncthreads();
+    if (tid < ROWS) {
+      const int s = slots[PIECE - 1 + tid], lead = tid - (s & (PIECE - 1));             // the row that would begin the row's piece
+      bool full = s >= 0;
+      for (int e = 0; e < PIECE; ++e) {
+        const int x = lead + e + PIECE - 1;
+        full = full && x < PIECE - 1 + ROWS && slots[x] == (s & ~(PIECE - 1)) + e;
+      }
+      kind[tid] = s < 0 ? 0 : full ? (lead == tid && tid < RA_WINDOW ? 1 : 0) : tid < RA_WINDOW ? 2 : 0;
+    }
+    __syncthreads();
+    // (lanes side by side have the pieces of one dim, which lie side by side in a block)
+    for (int i = tid; i < RA_WINDOW * hd; i += BLOCK) {
+      const int r = i & (RA_WINDOW - 1), d = i / RA_WINDOW;
+      if (kind[r] == 0) continue;
+      const int s = slots[PIECE - 1 + r];
+      T* dst = (T*)a.p.values + (((size_t)(s >> a.p.bt_shift) * a.p.nkv + head) * hd + d) * a.p.bt + (s & (a.p.bt - 1));
+      if (kind[r] == 2) {
+        *dst = vals[r][d];
+        continue;
+      }
+      __align__(16) T x[PIECE];
+#pragma unroll
+      for (int e = 0; e < PIECE; ++e) x[e] = vals[r + e][d];
+#pragma unroll
+      for (int e = 0; e < PIECE / N; ++e) ((u32x4*)dst)[e] = ((u32x4*)x)[e];
+    }
+    return;
+  }
+  const int half = hd >> 1, units = half / N, heads = a.nq + a.p.nkv, groups = (heads + RA_HEADS - 1) / RA_HEADS;
+  const long long i = (long long)(blockIdx.x - v_wgs) * BLOCK + tid;
+  const int row = (int)(i / (units * groups));
   if (row >= a.n_rows) return;
-  const int rest = (int)(i - (size_t)row * heads * half), h = rest / half, d = rest - h * half;
-  const int pos = a.row_pos[row], slot = a.row_slot[row];
-  const bool is_q = h < a.nq, is_k = !is_q && h < a.nq + a.p.nkv;
-  int bad = 0;
-  if (a.rope && pos >= a.positions) bad |= ST_BAD;
-  if (!is_q && slot >= 0 && (slot >> a.p.bt_shift) >= a.p.n_blocks) bad |= ST_PAGE;
-  if (bad) {
-    if (d == 0 && a.status) atomicOr(a.status, bad);
+  const int rest = (int)(i - (long long)row * (units * groups)), group = rest / units, d = (rest - group * units) * N;
+  const int pos = a.row_pos[row];
+  int slot = a.row_slot[row];
+  if (pos < 0) return;
+  if (a.rope && pos >= a.positions) {
+    if (rest == 0 && a.status) atomicOr(a.status, ST_BAD);
     return;
   }
-  if (pos < 0 || (!is_q && slot < 0)) return;
-  const T* src = is_q ? (const T*)a.q + row * a.q_stride + h * hd
-                      : is_k ? (const T*)a.k + row * a.k_stride + (h - a.nq) * hd : (const T*)a.v + row * a.v_stride + (h - a.nq - a.p.nkv) * hd;
-  const T x = src[d], y = src[d + half];
-  const size_t blk = (size_t)(slot >> a.p.bt_shift);
-  const int tok = slot & (a.p.bt - 1);
-  if (!is_q && !is_k) {
-    T* dst = (T*)a.p.values + (blk * a.p.nkv + (h - a.nq - a.p.nkv)) * hd * a.p.bt + tok;
-    dst[(size_t)d * a.p.bt] = x;
-    dst[(size_t)(d + half) * a.p.bt] = y;
-    return;
-  }
-  float c = 1.f, s = 0.f;
+  if (slot >= 0 && (slot >> a.p.bt_shift) >= a.p.n_blocks) slot = -1;      // (reported with the values)
+  float c[N], s[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) { c[e] = 1.f; s[e] = 0.f; }
   if (a.rope) {
-    const float* cs = a.rope + ((size_t)pos * half + d) * 2;
-    c = cs[0]; s = cs[1];
+    const f32x4* cs = (const f32x4*)(a.rope + ((size_t)pos * half + d) * 2);
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) {
+      const f32x4 v = cs[e];
+      c[2 * e] = v[0]; s[2 * e] = v[1]; c[2 * e + 1] = v[2]; s[2 * e + 1] = v[3];
+    }
   }
-  const float fx = DT::ld(&x), fy = DT::ld(&y);
-  T* dst = is_q ? (T*)a.q_out + row * a.q_out_stride + h * hd : (T*)a.p.keys + ((blk * a.p.nkv + (h - a.nq)) * a.p.bt + tok) * hd;
-  DT::st(dst + d, fx * c - fy * s);
-  DT::st(dst + d + half, fy * c + fx * s);
+#pragma unroll
+  for (int k = 0; k < RA_HEADS; ++k) {
+    const int h = group * RA_HEADS + k;
+    const bool is_q = h < a.nq;
+    if (h >= heads || (!is_q && slot < 0)) break;
+    const T* src = is_q ? (const T*)a.q + row * a.q_stride + h * hd : (const T*)a.k + row * a.k_stride + (h - a.nq) * hd;
+    T* dst = is_q ? (T*)a.q_out + row * a.q_out_stride + h * hd
+                  : (T*)a.p.keys + (((size_t)(slot >> a.p.bt_shift) * a.p.nkv + (h - a.nq)) * a.p.bt + (slot & (a.p.bt - 1))) * hd;
+    float x[N], y[N], u[N], w[N];
+    Unit<DT>::get(src + d, x);
+    Unit<DT>::get(src + d + half, y);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      u[e] = x[e] * c[e] - y[e] * s[e];
+      w[e] = y[e] * c[e] + x[e] * s[e];
+    }
+    Unit<DT>::put(dst + d, u);
+    Unit<DT>::put(dst + d + half, w);
+  }
 }
 
 }  // namespace ssd

@@ -65,6 +65,10 @@ extern "C" int ssd_block_tables(int n_seqs, int block_tokens, int n_blocks, int 
   a.B = n_seqs; a.bt_shift = log2_of(block_tokens); a.n_blocks = n_blocks; a.cap = table_cap; a.max_rows = max_rows;
   hipLaunchKernelGGL(k_block_tables, dim3(1), dim3(BT_THREADS), 0, (hipStream_t)stream, a);
   LAUNCH_CHECK();
+  if (max_rows > BT_ROWS_HERE) {
+    hipLaunchKernelGGL(k_block_table_rows, dim3(cdiv(max_rows, BLOCK)), dim3(BLOCK), 0, (hipStream_t)stream, a);
+    LAUNCH_CHECK();
+  }
   return SSD_OK;
 }
 
@@ -74,7 +78,9 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
   RopeAppendArgs a;
   if (int rc = check_pages(pages, a.p)) return rc;
   if (n_rows < 0 || n_rows > (1 << 24) || n_q_heads < 0 || n_q_heads > 1024) return fail(SSD_EINVAL, "bad n_rows / n_q_heads");
+  if (n_rows == 0) return SSD_OK;
   if (!dev_row_pos || !dev_row_slot) return fail(SSD_EINVAL, "null argument");
+  if (((uintptr_t)dev_rope & 15)) return fail(SSD_EINVAL, "the table of angles must be 16-byte aligned");
   if (dev_rope && rope_positions < 1) return fail(SSD_EINVAL, "rope_positions = %d", rope_positions);
   if (int rc = check_rows("k", dev_k, k_stride, a.p.nkv, a.p, pages->dtype)) return rc;
   if (int rc = check_rows("v", dev_v, v_stride, a.p.nkv, a.p, pages->dtype)) return rc;
@@ -82,15 +88,16 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
     if (int rc = check_rows("q", dev_q, q_stride, n_q_heads, a.p, pages->dtype)) return rc;
     if (int rc = check_rows("q_out", dev_q_out, q_out_stride, n_q_heads, a.p, pages->dtype)) return rc;
   }
-  if (n_rows == 0) return SSD_OK;
   a.q = dev_q; a.k = dev_k; a.v = dev_v; a.q_out = dev_q_out;
   a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.q_out_stride = q_out_stride;
   a.rope = dev_rope; a.row_pos = dev_row_pos; a.row_slot = dev_row_slot; a.status = dev_status;
   a.n_rows = n_rows; a.nq = n_q_heads; a.positions = rope_positions;
-  const long long n = (long long)n_rows * (n_q_heads + 2 * a.p.nkv) * (a.p.hd / 2);
-  const dim3 grid((unsigned)((n + BLOCK - 1) / BLOCK));
-  if (pages->dtype == SSD_DTYPE_BF16) hipLaunchKernelGGL(k_rope_append<BF16>, grid, dim3(BLOCK), 0, (hipStream_t)stream, a);
-  else hipLaunchKernelGGL(k_rope_append<F32>, grid, dim3(BLOCK), 0, (hipStream_t)stream, a);
+  const int per16 = pages->dtype == SSD_DTYPE_BF16 ? 8 : 4;
+  const int v_wgs = cdiv(n_rows, RA_WINDOW) * a.p.nkv;
+  const long long threads = (long long)n_rows * (a.p.hd / 2 / per16) * cdiv(n_q_heads + a.p.nkv, RA_HEADS);
+  const dim3 grid((unsigned)(v_wgs + (threads + BLOCK - 1) / BLOCK));
+  if (pages->dtype == SSD_DTYPE_BF16) hipLaunchKernelGGL(k_rope_append<BF16>, grid, dim3(BLOCK), 0, (hipStream_t)stream, a, v_wgs);
+  else hipLaunchKernelGGL(k_rope_append<F32>, grid, dim3(BLOCK), 0, (hipStream_t)stream, a, v_wgs);
   LAUNCH_CHECK();
   return SSD_OK;
 }
@@ -98,27 +105,36 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
 // ------------------------------------------------------------------------------------------------ attention
 // How a call is cut.  From sizes that the caller gives alone, so that the workspace's size is known without a device.
 struct AttnCut {
-  int sh_rows, own_rows;                                   // packed query rows of a workgroup: 16 (k_paged_attention), 128 or 256 (k_paged_tiles)
+  int qs, rt;                                              // 128 qs packed rows of a workgroup of paged_tiles, 16 rt of one of paged_stream; 0: none
+  bool in_line, own_tiles;
   int P, P_sh, sh_chunks, own_chunks, sh_slots, own_slots;
 };
 static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, int n_rows, int max_len, int shared_positions) {
+  constexpr int MAX_PARTS = 32;                            // of a source: 64 of a row
   AttnCut c;
-  const int packed = n_rows * group;
-  auto tile = [&](int rows) { return dtype != SSD_DTYPE_BF16 || rows < 48 ? 16 : hd == 128 || rows < 1024 ? 128 : 256; };
-  auto parts = [&](int tile, int slots, int keys) {
-    const int chunks = std::max(1, cdiv(keys, PA_CHUNK));
-    const int want = std::max(1, (tile > 16 ? 512 : 1024) / std::max(1, slots * nkv));
-    return std::max(1, std::min({want, cdiv(chunks, 4), 64}));
+  const bool b16 = dtype == SSD_DTYPE_BF16;
+  const int packed = n_rows * group, each = cdiv(packed, n_seqs), max_rt = hd == 128 ? 2 : 3;
+  c.in_line = n_seqs == 1 || each >= 256;
+  const bool apart = shared_positions > 0 && !c.in_line;
+  c.own_tiles = b16 && each >= 48;
+  const bool sh_tiles = b16 && apart && packed >= 48;
+  c.qs = !c.own_tiles && !sh_tiles ? 0 : hd < 128 && (c.own_tiles ? each : packed) >= 512 ? 2 : 1;
+  c.rt = c.own_tiles ? 0 : each <= 16 ? 1 : max_rt;
+  const int own_t = c.own_tiles ? 128 * c.qs : 16 * c.rt, sh_t = sh_tiles ? 128 * c.qs : 16 * c.rt;
+  // parts: as many as give every compute unit work, of no fewer than `least` chunks
+  auto parts = [&](int slots, int keys, int wgs, int least) {
+    return std::max(1, std::min({wgs / std::max(1, slots * nkv), cdiv(std::max(1, cdiv(keys, PA_CHUNK)), least), MAX_PARTS}));
   };
-  c.sh_rows = tile(packed);
-  c.own_rows = tile(packed / n_seqs);
-  c.own_slots = packed / c.own_rows + n_seqs;
-  c.sh_slots = shared_positions ? cdiv(packed, c.sh_rows) : 0;
-  const int own = std::max(1, max_len - shared_positions), own_parts = parts(c.own_rows, std::max(n_seqs, packed / c.own_rows), own);
+  c.own_slots = packed / own_t + n_seqs;
+  c.sh_slots = apart ? cdiv(packed, sh_t) : 0;
+  const int own = std::max(1, max_len - (apart ? shared_positions : 0)), own_parts = parts(std::max(n_seqs, packed / own_t), own, c.own_tiles ? 512 : 1024, 4);
   c.own_chunks = cdiv(cdiv(own, PA_CHUNK), own_parts);
-  c.P_sh = shared_positions ? parts(c.sh_rows, c.sh_slots, shared_positions) : 0;
-  c.sh_chunks = c.P_sh ? cdiv(cdiv(shared_positions, PA_CHUNK), c.P_sh) : 0;
-  if (c.P_sh) c.P_sh = cdiv(cdiv(shared_positions, PA_CHUNK), c.sh_chunks);
+  c.P_sh = c.sh_chunks = 0;
+  if (apart) {
+    const int chunks = cdiv(shared_positions, PA_CHUNK);
+    c.sh_chunks = cdiv(chunks, parts(c.sh_slots, shared_positions, sh_tiles ? 512 : 1024, 4));
+    c.P_sh = cdiv(chunks, c.sh_chunks);
+  }
   c.P = c.P_sh + own_parts;
   return c;
 }
@@ -138,34 +154,28 @@ extern "C" size_t ssd_paged_attention_workspace_bytes(const ssd_pages* pages, in
   return attention_ws(cut_attention(pages->dtype, p.hd, p.nkv, n_q_heads / p.nkv, n_seqs, n_rows, max_len, shared_blocks * p.bt), n_rows, n_q_heads, p.hd);
 }
 
-// `rows`: packed query rows of a workgroup; `shared`, `own`: which sources of keys this launch takes.
-template <typename DT, int HD>
-static int launch_paged_source(PagedAttnArgs a, int rows, bool shared, bool own, hipStream_t st) {
-  if (!shared) a.sh_slots = 0;
-  if (!own) a.own_slots = 0;
+template <typename DT, int HD, int QS, int RT>
+static int launch_attention(const PagedAttnArgs& a, hipStream_t st) {
   const long long wgs = ((long long)a.sh_slots * a.P_sh + (long long)a.own_slots * (a.P - a.P_sh)) * a.p.nkv;
-  if (wgs == 0) return SSD_OK;
   if (wgs > 0x7FFFFFFFll) return fail(SSD_ENOSUP, "too many workgroups");
-  if constexpr (std::is_same<DT, BF16>::value) {
-    if (rows == 128) hipLaunchKernelGGL((k_paged_tiles<HD, 1>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
-    if constexpr (HD < 128)
-      if (rows == 256) hipLaunchKernelGGL((k_paged_tiles<HD, 2>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
-  }
-  if (rows == 16) hipLaunchKernelGGL((k_paged_attention<DT, HD>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
+  hipLaunchKernelGGL((k_paged_attention<DT, HD, QS, RT>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
   LAUNCH_CHECK();
+  if (a.P > 1) {
+    hipLaunchKernelGGL((k_paged_attention_merge<DT, HD>), dim3((unsigned)cdiv(a.n_rows * a.nq, BLOCK / WAVE)), dim3(BLOCK), 0, st, a);
+    LAUNCH_CHECK();
+  }
   return SSD_OK;
 }
 template <typename DT, int HD>
 static int launch_paged_attention(const PagedAttnArgs& a, const AttnCut& c, hipStream_t st) {
-  const bool one = c.sh_rows == c.own_rows;
-  if (int rc = launch_paged_source<DT, HD>(a, c.own_rows, one, true, st)) return rc;
-  if (!one)
-    if (int rc = launch_paged_source<DT, HD>(a, c.sh_rows, true, false, st)) return rc;
-  if (a.P > 1) {
-    hipLaunchKernelGGL((k_paged_attention_merge<DT, HD>), dim3((unsigned)((a.n_rows * a.nq + 3) / 4)), dim3(BLOCK), 0, st, a);
-    LAUNCH_CHECK();
+  constexpr int MANY = HD == 128 ? 2 : 3;
+  if constexpr (std::is_same<DT, BF16>::value) {
+    if constexpr (HD < 128) {
+      if (c.qs == 2) return c.rt == 0 ? launch_attention<DT, HD, 2, 0>(a, st) : c.rt == 1 ? launch_attention<DT, HD, 2, 1>(a, st) : launch_attention<DT, HD, 2, MANY>(a, st);
+    }
+    if (c.qs == 1) return c.rt == 0 ? launch_attention<DT, HD, 1, 0>(a, st) : c.rt == 1 ? launch_attention<DT, HD, 1, 1>(a, st) : launch_attention<DT, HD, 1, MANY>(a, st);
   }
-  return SSD_OK;
+  return c.rt == 1 ? launch_attention<DT, HD, 0, 1>(a, st) : launch_attention<DT, HD, 0, MANY>(a, st);
 }
 
 extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float scale, int n_seqs, int n_rows, int max_len, const int32_t* dev_len,
@@ -174,12 +184,12 @@ extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float 
                                    size_t ws_bytes, int32_t* dev_status, void* stream) {
   PagedAttnArgs a;
   if (int rc = check_attention(pages, a.p, n_q_heads, n_seqs, n_rows, max_len, shared_blocks)) return rc;
+  if (n_rows == 0) return SSD_OK;
   if (!dev_len || !dev_row_start || !dev_table || (shared_blocks > 0 && !dev_shared_table)) return fail(SSD_EINVAL, "null argument");
   if (table_cap < 1 || (long long)table_cap * a.p.bt > (1 << 30)) return fail(SSD_EINVAL, "table_cap = %d", table_cap);
   if (!std::isfinite(scale)) return fail(SSD_EINVAL, "scale is not finite");
   if (int rc = check_rows("q", dev_q, q_stride, n_q_heads, a.p, pages->dtype)) return rc;
   if (int rc = check_rows("out", dev_out, out_stride, n_q_heads, a.p, pages->dtype)) return rc;
-  if (n_rows == 0) return SSD_OK;
   const AttnCut c = cut_attention(pages->dtype, a.p.hd, a.p.nkv, n_q_heads / a.p.nkv, n_seqs, n_rows, max_len, shared_blocks * a.p.bt);
   const size_t need = attention_ws(c, n_rows, n_q_heads, a.p.hd);
   if (need && (!dev_ws || ((uintptr_t)dev_ws & 15))) return fail(SSD_EINVAL, "workspace is null or not 16-byte aligned");
@@ -190,6 +200,9 @@ extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float 
   a.ml_part = a.o_part + (size_t)n_rows * n_q_heads * c.P * a.p.hd;
   a.scale2 = scale * 1.44269504088896340736f;
   a.nq = n_q_heads; a.n_seqs = n_seqs; a.n_rows = n_rows; a.cap = table_cap; a.shared_blocks = shared_blocks;
+  a.in_line = c.in_line && shared_blocks > 0;
+  a.tile_wgs = c.qs ? c.sh_slots * c.P_sh * a.p.nkv + (c.own_tiles ? c.own_slots * (c.P - c.P_sh) * a.p.nkv : 0) : 0;
+  a.own_tiles = c.own_tiles;
   a.P = c.P; a.P_sh = c.P_sh; a.sh_chunks = c.sh_chunks; a.own_chunks = c.own_chunks; a.sh_slots = c.sh_slots; a.own_slots = c.own_slots;
   hipStream_t st = (hipStream_t)stream;
   const bool b16 = pages->dtype == SSD_DTYPE_BF16;
