@@ -6,7 +6,7 @@
 //
 // Two ways of taking a source of keys, whose query rows - rows x the G query heads of a kv head, packed [row][head] - share them:
 //   paged_tiles   128 or 256 packed rows a workgroup, keys and values through LDS: the shared prefix, prompts
-//   paged_stream  up to 64 packed rows, keys and values straight into registers: a sequence's own keys while it decodes or verifies; fp32
+//   paged_stream  up to 32 packed rows, keys and values straight into registers: a sequence's own keys while it decodes or verifies; fp32
 // and one launch has workgroups of both, so that the products of the one run beside the loads of the other.
 //
 // Scores and outputs are computed transposed (S^T = K Q^T, O^T = V^T P^T): a lane holds scores and outputs of one query row, the weights go from the
@@ -16,6 +16,8 @@
 // The bf16 kernels round the weights to bf16 for the second product (2^-9 of each on average, at random: the sum is off by about as much as the
 // output's own rounding); their sum is taken of the unrounded ones, in fp32.
 #pragma once
+#include <type_traits>
+
 #include "common.h"
 #include "pages.h"
 
@@ -23,7 +25,8 @@ namespace ssd {
 
 constexpr int PA_WAVES = 4, PA_THREADS = PA_WAVES * WAVE;
 constexpr int PA_CHUNK = 64;           // keys in which parts are counted
-constexpr float PA_LAZY = 8.0f, PA_NONE = -3.0e38f;      // the second: the reference of a row that has seen nothing
+constexpr float PA_LAZY = 8.0f, PA_LARGE = 256.0f;
+constexpr float PA_NONE = -3.0e38f;    // the reference of a row that has seen nothing
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 struct PagedAttnArgs {
@@ -41,8 +44,8 @@ struct PagedAttnArgs {
   int P, P_sh;           // parts of a row at most, and those of the shared prefix
   int sh_chunks;         // chunks of a part of the shared prefix
   int own_chunks;        // chunks of a part of a sequence's keys, at least
-  int tile_wgs;          // workgroups of paged_tiles: sh_slots x P_sh x nkv of the shared prefix, and then, if own_tiles, own_slots x (P - P_sh) x nkv
-  int sh_slots, own_slots, own_tiles;
+  int sh_slots, own_slots;             // tiles of query rows of the shared prefix, of the sequences: workgroups are sh_slots x P_sh x nkv and then own_slots x (P - P_sh) x nkv
+  int by_length;         // 1: the sequences' tiles in descending order of length
 };
 
 struct SeqRows {
@@ -92,6 +95,20 @@ __device__ __forceinline__ bool shared_work(const PagedAttnArgs& a, int id, int 
   w.shared = true;
   return w.row0 < w.n_packed;
 }
+// A tile of sequence s against a part of its keys.
+__device__ __forceinline__ void own_tile(const PagedAttnArgs& a, const SeqRows& r, int s, int row0, int part, int T, int G, Work& w) {
+  w.row0 = row0;
+  w.n_packed = r.n * G;
+  w.table = a.table + (size_t)s * a.cap;
+  w.table_n = a.cap;
+  w.head = r.head;
+  w.seq_r0 = r.r0;
+  w.len = r.len;
+  w.k_begin = r.start + part * r.per * PA_CHUNK;
+  w.k_end = min(r.len + min(r.n - 1, (row0 + T - 1) / G) + 1, w.k_begin + r.per * PA_CHUNK);        // (up to the last position that a row of the tile sees)
+  w.slot = r.chunks <= r.per && r.start == 0 ? -1 : a.P_sh + part;
+  w.shared = false;
+}
 __device__ __forceinline__ bool own_work(const PagedAttnArgs& a, int id, int T, int G, Work& w) {
   const int parts = a.P - a.P_sh, slot = id / parts, part = id - slot * parts;
   // (sequence s has tiles from r0 G / T + s on: room for a last one that is not full, without a list of tiles)
@@ -104,18 +121,60 @@ __device__ __forceinline__ bool own_work(const PagedAttnArgs& a, int id, int T, 
     if (threadIdx.x == 0 && a.status) atomicOr(a.status, ST_BAD);
     return false;
   }
-  const int n = ceil_div(r.chunks, r.per);
-  if (part >= n) return false;
-  w.table = a.table + (size_t)s * a.cap;
-  w.table_n = a.cap;
-  w.head = r.head;
-  w.seq_r0 = r.r0;
-  w.len = r.len;
-  w.k_begin = r.start + part * r.per * PA_CHUNK;
-  w.k_end = min(r.len + min(r.n - 1, (w.row0 + T - 1) / G) + 1, w.k_begin + r.per * PA_CHUNK);      // (up to the last position that a row of the tile sees)
-  w.slot = n == 1 && r.start == 0 ? -1 : a.P_sh + part;
-  w.shared = false;
+  if (part >= ceil_div(r.chunks, r.per)) return false;
+  own_tile(a, r, s, w.row0, part, T, G, w);
   return true;
+}
+// The same for launches in which every sequence is one part, the longest tiles first: workgroups that are given out last, to compute units that are done, have the
+// least to do.  (Tiles of a sequence ascend in length: how many have at least c chunks is a quotient, and a search over c finds the length of the tile
+// with `rank` longer ones or equals before it.)
+__device__ __forceinline__ bool own_work_by_length(const PagedAttnArgs& a, int rank, int T, int G, Work& w) {
+  const int lane = threadIdx.x & 63;
+  auto tiles = [&](const SeqRows& r) { return r.ok ? ceil_div(r.n * G, T) : 0; };
+  auto first_of = [&](const SeqRows& r, int c) {           // the first tile of at least c chunks
+    const int row = (c - 1) * PA_CHUNK + r.start - r.len;  // whose last row is this one or a later one
+    return row <= 0 ? 0 : row >= r.n ? tiles(r) : row * G / T;
+  };
+  auto count = [&](int c) {                                // (fewer than 2^24: exact)
+    int n = 0;
+    for (int s = lane; s < a.n_seqs; s += 64) {
+      const SeqRows r = seq_rows(a, s);
+      n += tiles(r) - first_of(r, c);
+    }
+    return (int)wave_sum((float)n);
+  };
+  int bad = 0, longest = 0;
+  for (int s = lane; s < a.n_seqs; s += 64) {
+    const SeqRows r = seq_rows(a, s);
+    bad |= r.n > 0 && !r.ok;
+    longest = max(longest, r.ok ? r.chunks : 0);
+  }
+  if (rank == 0 && bad && a.status) atomicOr(a.status, ST_BAD);
+  int lo = 0, hi = (int)wave_max((float)longest) + 1;      // more than `rank` tiles have at least lo chunks (any have 0), no more than that have hi (fewer than 2^24: exact)
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (count(mid) > rank) lo = mid; else hi = mid;
+  }
+  if (lo == 0) return false;
+  int left = rank - count(hi);                             // which of the tiles of lo chunks
+  for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
+    int n = 0, first = 0;
+    if (s0 + lane < a.n_seqs) {
+      const SeqRows r = seq_rows(a, s0 + lane);
+      first = first_of(r, lo);
+      n = first_of(r, hi) - first;
+    }
+    const int upto = (int)wave_inclusive_scan((unsigned)n);
+    const unsigned long long m = __ballot(upto > left);
+    if (m) {
+      const int l = __builtin_ctzll(m);
+      const int s = s0 + l, tile = __builtin_amdgcn_readlane(first, l) + left - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l));
+      own_tile(a, seq_rows(a, s), s, tile * T, 0, T, G, w);
+      return w.row0 < w.n_packed;
+    }
+    left -= __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
 }
 // The block of key `key`, as the table has it; -1 behind the last key and the table's end.
 __device__ __forceinline__ int block_of(const PagedAttnArgs& a, const Work& w, int key) {
@@ -149,7 +208,7 @@ struct StreamShape {
   static constexpr int LDS = PA_WAVES * 16 * (HD + 4) + 2 * PA_WAVES * 16;         // floats
 };
 
-template <typename DT, int HD, int RT>
+template <typename DT, int HD, int RT, bool SHARED>
 __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, float* lds) {
   typedef typename DT::T T;
   typedef StreamShape<DT, HD> S;
@@ -159,8 +218,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
   const int nkv = a.p.nkv, G = a.nq / nkv, kvh = id % nkv, tmask = a.p.bt - 1;
   id /= nkv;
   Work w;
-  const int sh = a.tile_wgs ? 0 : a.sh_slots * a.P_sh;     // (the shared prefix is paged_tiles' if there are any)
-  if (!(id < sh ? shared_work(a, id, 16 * RT, G, w) : own_work(a, id - sh, 16 * RT, G, w))) return;
+  if (!(SHARED ? shared_work(a, id, 16 * RT, G, w) : own_work(a, id, 16 * RT, G, w))) return;
   const int rows = min(16 * RT, w.n_packed - w.row0);      // (uniform: tiles behind the last row are left out)
   const int pos_lo = w.shared ? 0x7FFFFFFF : w.len + w.row0 / G;
   // block ids of the wave's next 64 / NT steps: lane NT i + t has that of tile t of step i
@@ -364,39 +422,46 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
 // loads put them a chunk ahead (wave w the 16 keys w of a chunk, which lie in one block).  32x32x16 products: a lane holds the scores of one row
 // (lane % 32) for keys 16 (i / 8) + 8 h + i % 8 of a 32-key tile (i: register, h = lane / 32) if row m of the tile's operand is the key whose bits 2 and 3
 // are those of m swapped; these are the operand of the second product as they stand.
-//   LDS of a chunk, 1 KB for each direct load: keys [group of 16][32 dims][8-dim piece][key], values [group of 16][32 dims][8-key half][dim].
+//   A direct load brings 1 KB of consecutive memory where the layout has it, so keys are parked [group of 16][key][16-byte unit] and values [group of
+// 16][dim][8-key half], with unit u of key t at u ^ (t >> (4 - log2 units)) and half x of dim d at x ^ (d >> 3 & 1): the sixteen lanes of a read then
+// have sixteen distinct quads of banks.
 template <int HD>
 struct TileShape {
   static constexpr int J = HD / 32;
-  typedef u32x4 Lds[2][2][4][J][64];   // [buffer][keys, values][group][32 dims][..]
+  typedef u32x4 Lds[2][2][4][J][64];   // [buffer][keys, values][group][..]
 };
 
-template <int HD, int QS>
+template <int HD, int QS, bool SHARED>
 __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, typename TileShape<HD>::Lds& kv_lds) {
   constexpr int J = HD / 32, T = 128 * QS;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
   const int nkv = a.p.nkv, G = a.nq / nkv, kvh = id % nkv, tmask = a.p.bt - 1;
   id /= nkv;
   Work w;
-  const int sh = a.sh_slots * a.P_sh;
-  if (!(id < sh ? shared_work(a, id, T, G, w) : own_work(a, id - sh, T, G, w))) return;
+  if (!(SHARED ? shared_work(a, id, T, G, w) : a.by_length ? own_work_by_length(a, id, T, G, w) : own_work(a, id, T, G, w))) return;
   const int n_chunks = max(0, ceil_div(w.k_end - w.k_begin, PA_CHUNK));
   // this wave's rows and what they see
   const int w0 = w.row0 + wave * 32 * QS;
   const bool has_rows = w0 < w.n_packed;
-  const int pos_lo = w.shared ? 0x7FFFFFFF : w.len + w0 / G, reach = w.shared ? 0x7FFFFFFF : w.len + (min(w0 + 32 * QS, w.n_packed) - 1) / G;
-  int pos[QS];
-  size_t at[QS];                                           // row * nq + head
+  const int reach = !has_rows ? -1 : w.shared ? 0x7FFFFFFF : w.len + (min(w0 + 32 * QS, w.n_packed) - 1) / G;
+  const int full_to = min(w.k_end, w.shared ? 0x7FFFFFFF : w.len + w0 / G + 1);        // keys before this one are there for all of the wave's rows
+  // block ids of 16 chunks at a time: lane i has that of keys 16 i .. of them; and the next 16 chunks', looked at when their turn comes
+  int bad = 0;
+  auto key_of = [&](int chunk) { return w.k_begin + chunk * PA_CHUNK + lane * 16; };
+  int ids = block_of(a, w, key_of(0)), ids_next = block_of(a, w, key_of(16));
+  int row[QS], head[QS];
   bf16x8 q[QS][2 * J];
 #pragma unroll
   for (int x = 0; x < QS; ++x) {
-    const int pr = min(w0 + 32 * x + c, w.n_packed - 1), row = w.seq_r0 + pr / G, head = kvh * G + pr % G;
-    pos[x] = w.shared ? 0x7FFFFFFF : w.len + pr / G;
-    at[x] = (size_t)row * a.nq + head;
-    const u32x4* qp = (const u32x4*)((const bf16_t*)a.q + row * a.q_stride + head * HD) + h;
+    const int pr = min(w0 + 32 * x + c, w.n_packed - 1);
+    row[x] = w.seq_r0 + pr / G;
+    head[x] = kvh * G + pr % G;
+    const u32x4* qp = (const u32x4*)((const bf16_t*)a.q + row[x] * a.q_stride + head[x] * HD) + h;
 #pragma unroll
     for (int s = 0; s < 2 * J; ++s) q[x][s] = __builtin_bit_cast(bf16x8, qp[2 * s]);
   }
+  ids = checked_block(a, w, ids, key_of(0), bad);
+  unsigned long long have = __ballot(ids >= 0);            // a bit for each group of 16 keys whose block is there
   const float scale2 = factor(a);
   if (a.scale2 <= 0.f) {
 #pragma unroll
@@ -404,24 +469,30 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
 #pragma unroll
       for (int s = 0; s < 2 * J; ++s) q[x][s] = __builtin_bit_cast(bf16x8, factor_into(a, __builtin_bit_cast(u32x4, q[x][s]), 0x80008000u));
   }
-  // block ids of 16 chunks at a time: lane i has that of keys 16 i .. of them; and the next 16 chunks', looked at when their turn comes
-  int bad = 0;
-  auto key_of = [&](int chunk) { return w.k_begin + chunk * PA_CHUNK + lane * 16; };
-  int ids = checked_block(a, w, block_of(a, w, key_of(0)), key_of(0), bad), ids_next = block_of(a, w, key_of(16));
-  const int k_lane = ((lane & 15) * HD + (lane >> 4) * 8) * 2, v_lane = (c * a.p.bt + h * 8) * 2;
-  const size_t head_bytes = (size_t)a.p.bt * HD * 2;
-  auto request = [&](int it) {                             // returns which of the chunk's groups are there
-    if (it && it % 16 == 0) { ids = checked_block(a, w, ids_next, key_of(it), bad); ids_next = block_of(a, w, key_of(it + 16)); }
-    const int blk = __builtin_amdgcn_readlane(ids, (it & 15) * 4 + wave);
-    const int tok = (w.k_begin + it * PA_CHUNK + wave * 16) & tmask;
-    const size_t at_ = ((size_t)max(blk, 0) * nkv + kvh) * head_bytes;
-    const rsrc_t rk = load_rsrc((const char*)a.p.keys + at_ + tok * HD * 2), rv = load_rsrc((const char*)a.p.values + at_ + tok * 2);
+  // units of a key; a load's lanes have keys t, t + 64 / UNITS, ..
+  constexpr int UNITS = HD / 8, SW = UNITS == 4 ? 2 : UNITS == 8 ? 1 : 0;
+  int k_off[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) load_to_lds(rk, &kv_lds[it & 1][0][wave][j][0], k_lane, j * 64);
+  for (int j = 0; j < J; ++j) {
+    const int t = j * (64 / UNITS) + lane / UNITS;
+    k_off[j] = (t * HD + ((lane % UNITS) ^ (t >> SW & (UNITS - 1))) * 8) * 2;
+  }
+  const int v_half = (lane & 1) ^ (lane >> 4 & 1), v_off = ((lane >> 1) * a.p.bt + v_half * 8) * 2, v_dims = 32 * a.p.bt * 2;
+  const uint32_t head_bytes = (uint32_t)a.p.bt * HD * 2, block_bytes = head_bytes * nkv;            // (< 2^28)
+  const char* keys = (const char*)a.p.keys + (size_t)kvh * head_bytes;
+  const char* values = (const char*)a.p.values + (size_t)kvh * head_bytes;
+  int tok = (w.k_begin + wave * 16) & tmask;               // of this wave's group of the chunk that is requested next
+  auto request = [&](int it) {
+    const uint32_t blk = (uint32_t)max(__builtin_amdgcn_readlane(ids, (it & 15) * 4 + wave), 0);
+    const size_t at = (size_t)blk * block_bytes;
+    const rsrc_t rk = load_rsrc(keys + at + tok * (HD * 2)), rv = load_rsrc(values + at + tok * 2);
 #pragma unroll
-    for (int j = 0; j < J; ++j) load_to_lds(rv, &kv_lds[it & 1][1][wave][j][0], v_lane + j * 32 * a.p.bt * 2, 0);
-    return (int)(__ballot(ids >= 0) >> ((it & 15) * 4)) & 15;
+    for (int j = 0; j < J; ++j) load_to_lds(rk, &kv_lds[it & 1][0][wave][j][0], k_off[j], 0);
+#pragma unroll
+    for (int j = 0; j < J; ++j) load_to_lds(rv, &kv_lds[it & 1][1][wave][j][0], v_off, j * v_dims);
+    tok = (tok + PA_CHUNK) & tmask;
   };
+  const int kk = (c & 19) | (c & 4) << 1 | (c & 8) >> 1;   // the key that row c of a tile's operand is
   f32x16 o[QS][J];
   float m[QS], l[QS];
 #pragma unroll
@@ -433,101 +504,126 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[x][d][i] = 0.f;
   }
-  const int kk = (c & ~12) | (c & 4) << 1 | (c & 8) >> 1;  // the key that row c of a tile's operand is
-  int there = n_chunks ? request(0) : 0;
+  if (n_chunks > 0) request(0);
   for (int it = 0; it < n_chunks; ++it) {
     const int kbase = w.k_begin + it * PA_CHUNK;
+    const int now = (int)(have >> ((it & 15) * 4)) & 15;
     // (the builtin: with a wait in assembly the compiler places waits of its own for the queries, and with them for the chunk that was just requested)
-    __builtin_amdgcn_s_waitcnt(0x0070);                    // vmcnt(0) lgkmcnt(0)
-    asm volatile("" ::: "memory");                         // (the chunk has arrived; and nothing is still to be read of the one whose buffer is next)
-    // values of this wave's group that are not there may be anything: they become zeros
-    const int n_tok = (there >> wave & 1) ? w.k_end - (kbase + wave * 16) : 0;
-    if (n_tok < 16) {
+    __builtin_amdgcn_s_waitcnt(0x0070);                    // vmcnt(0) lgkmcnt(0): the chunk has arrived, and nothing is still to be read of the one whose buffer is next
+    asm volatile("" ::: "memory");
+    if (now != 15 || kbase + PA_CHUNK > w.k_end) {
+      // values of this wave's group that are not there may be anything: they become zeros
+      const int n_tok = (now >> wave & 1) ? w.k_end - (kbase + wave * 16) : 0;
+      if (n_tok < 16) {
 #pragma unroll
-      for (int j = 0; j < J; ++j) {
-        u32x4 v = kv_lds[it & 1][1][wave][j][lane];
-        const int n = n_tok - 8 * h;
+        for (int j = 0; j < J; ++j) {
+          u32x4 v = kv_lds[it & 1][1][wave][j][lane];
+          const int n = n_tok - 8 * v_half;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] &= (2 * e < n ? 0xFFFFu : 0u) | (2 * e + 1 < n ? 0xFFFF0000u : 0u);
-        kv_lds[it & 1][1][wave][j][lane] = v;
+          for (int e = 0; e < 4; ++e) v[e] &= (2 * e < n ? 0xFFFFu : 0u) | (2 * e + 1 < n ? 0xFFFF0000u : 0u);
+          kv_lds[it & 1][1][wave][j][lane] = v;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    const int now = there;
-    if (it + 1 < n_chunks) there = request(it + 1);
-    if (!has_rows || kbase > reach) continue;
-    const bool edge = now != 15 || kbase + PA_CHUNK > w.k_end || kbase + PA_CHUNK - 1 > pos_lo;
-    f32x16 s[QS][2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int x = 0; x < QS; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[x][t][i] = 0.f;
-#pragma unroll
-      for (int k = 0; k < 2 * J; ++k) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, kv_lds[it & 1][0][2 * t + (kk >> 4)][k >> 1][((k & 1) * 2 + h) * 16 + (kk & 15)]);
-#pragma unroll
-        for (int x = 0; x < QS; ++x) s[x][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[x][k], s[x][t], 0, 0, 0);
+    if (it + 1 < n_chunks) {
+      if ((it & 15) == 15) {
+        ids = checked_block(a, w, ids_next, key_of(it + 1), bad);
+        have = __ballot(ids >= 0);
+        ids_next = block_of(a, w, key_of(it + 17));
       }
+      request(it + 1);
     }
-    if (edge) {
+    if (kbase > reach) continue;
+    const bool edge = now != 15 || kbase + PA_CHUNK > full_to;
+    // Weights by the references that the rows have; if some row's come out too large - the first chunk's always do - they are taken again, after a look at the
+    // largest scores, from the keys, which are still at hand.
+    bf16x8 p[QS][4];
+    float sum[QS];
+    auto weigh = [&](auto look) {
+      f32x16 s[QS][2];
 #pragma unroll
-      for (int x = 0; x < QS; ++x) {
-        const int last = min(pos[x], w.k_end - 1) - kbase - 8 * h;           // of this lane's keys, less 8 h
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int x = 0; x < QS; ++x)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[x][t][i] = 0.f;
+      bf16x8 kf[2 * J][2];
+#pragma unroll
+      for (int k = 0; k < 2 * J; ++k)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          kf[k][t] = __builtin_bit_cast(bf16x8, (&kv_lds[it & 1][0][2 * t + (kk >> 4)][0][0])[(kk & 15) * UNITS + ((2 * k + h) ^ ((kk & 15) >> SW & (UNITS - 1)))]);
+#pragma unroll
+      for (int k = 0; k < 2 * J; ++k)                      // (chains side by side, or each product waits for the one before)
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = 32 * t + 16 * (i >> 3) + (i & 7);
-            if (key > last || !(now >> (2 * t + (i >> 3)) & 1)) s[x][t][i] = -INFINITY;
+          for (int x = 0; x < QS; ++x) s[x][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][t], q[x][k], s[x][t], 0, 0, 0);
+      if (edge) {
+#pragma unroll
+        for (int x = 0; x < QS; ++x) {
+          const int pos = w.shared ? 0x7FFFFFFF : w.len + row[x] - w.seq_r0;
+          const int last = min(pos, w.k_end - 1) - kbase - 8 * h;            // of this lane's keys, less 8 h
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            int last_y = now >> y & 1 ? last : -1;
+            asm volatile("" : "+v"(last_y));                                 // (or the comparisons are made for every chunk)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (16 * y + i > last_y) s[x][y >> 1][(y & 1) * 8 + i] = -INFINITY;
           }
-      }
-    }
-    bf16x8 p[QS][4];
-#pragma unroll
-    for (int x = 0; x < QS; ++x) {
-      float mx = s[x][0][0];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][t][i]);
-      mx *= scale2;
-      if (__any(mx > m[x] + PA_LAZY)) {
-        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-        mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-        if (mx > m[x] + PA_LAZY) {
-          const float keep = __builtin_amdgcn_exp2f(m[x] - mx);
-          m[x] = mx;
-          l[x] *= keep;
-#pragma unroll
-          for (int d = 0; d < J; ++d) o[x][d] *= keep;
         }
       }
-      float sum = 0.f;
+      if constexpr (decltype(look)::value) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+        for (int x = 0; x < QS; ++x) {
+          float mx = s[x][0][0];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[x][t][i] = __builtin_amdgcn_exp2f(fmaf(s[x][t][i], scale2, -m[x]));
-          sum += s[x][t][i];
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][t][i]);
+          const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+          mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * scale2;
+          if (mx > m[x]) {
+            const float keep = __builtin_amdgcn_exp2f(m[x] - mx);
+            m[x] = mx;
+            l[x] *= keep;
+#pragma unroll
+            for (int d = 0; d < J; ++d) o[x][d] *= keep;
+          }
         }
-      l[x] += sum;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        u32x4 w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = f2_to_bf16x2(s[x][k >> 1][(k & 1) * 8 + 2 * e], s[x][k >> 1][(k & 1) * 8 + 2 * e + 1]);
-        p[x][k] = __builtin_bit_cast(bf16x8, w);
       }
-    }
+      bool large = false;
+#pragma unroll
+      for (int x = 0; x < QS; ++x) {
+        sum[x] = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          u32x4 w4;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int i = (k & 1) * 8 + 2 * e;
+            const uint32_t two = f2_to_bf16x2(__builtin_amdgcn_exp2f(fmaf(s[x][k >> 1][i], scale2, -m[x])), __builtin_amdgcn_exp2f(fmaf(s[x][k >> 1][i + 1], scale2, -m[x])));
+            w4[e] = two;                                   // (a bit cast of a vector's element is one of its first)
+            sum[x] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, two), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), sum[x], false);
+          }
+          p[x][k] = __builtin_bit_cast(bf16x8, w4);
+        }
+        large |= !(sum[x] <= PA_LARGE);
+      }
+      return __any(large) != 0;
+    };
+    if (it == 0 || weigh(std::false_type())) weigh(std::true_type());
+#pragma unroll
+    for (int x = 0; x < QS; ++x) l[x] += sum[x];
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
       for (int d = 0; d < J; ++d) {
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, kv_lds[it & 1][1][k][d][lane]);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, kv_lds[it & 1][1][k][d][2 * c + (h ^ (c >> 3 & 1))]);
 #pragma unroll
         for (int x = 0; x < QS; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[x][k], o[x][d], 0, 0, 0);
       }
@@ -541,37 +637,43 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
     // dims 32 d + 8 e + 4 h .. + 3 in registers 4 e ..
     if (w.slot < 0) {
       const float inv = ls == 0.f ? 0.f : 1.f / ls;
-      const size_t row = at[x] / a.nq, head = at[x] - row * a.nq;
-      bf16_t* dst = (bf16_t*)a.out + row * a.out_stride + head * HD + 4 * h;
+      bf16_t* dst = (bf16_t*)a.out + row[x] * a.out_stride + head[x] * HD + 4 * h;
 #pragma unroll
       for (int d = 0; d < J; ++d)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *(uint2*)(dst + 32 * d + 8 * e) = make_uint2(f2_to_bf16x2(o[x][d][4 * e] * inv, o[x][d][4 * e + 1] * inv), f2_to_bf16x2(o[x][d][4 * e + 2] * inv, o[x][d][4 * e + 3] * inv));
     } else {
-      float* dst = a.o_part + (at[x] * a.P + w.slot) * HD + 4 * h;
+      const size_t at = ((size_t)row[x] * a.nq + head[x]) * a.P + w.slot;
+      float* dst = a.o_part + at * HD + 4 * h;
 #pragma unroll
       for (int d = 0; d < J; ++d)
 #pragma unroll
         for (int e = 0; e < 4; ++e) *(f32x4*)(dst + 32 * d + 8 * e) = f32x4{o[x][d][4 * e], o[x][d][4 * e + 1], o[x][d][4 * e + 2], o[x][d][4 * e + 3]};
-      if (h == 0) { a.ml_part[(at[x] * a.P + w.slot) * 2] = m[x]; a.ml_part[(at[x] * a.P + w.slot) * 2 + 1] = ls; }
+      if (h == 0) { a.ml_part[at * 2] = m[x]; a.ml_part[at * 2 + 1] = ls; }
     }
   }
 }
 
-// The first tile_wgs workgroups are paged_tiles', the others paged_stream's.  QS or RT 0: a launch without them.
-template <typename DT, int HD, int QS, int RT>
+// The shared prefix first: its workgroups have the most to do.  SH: by tiles of 128 or 256 rows (1, 2), by streams (3), none (0); OWN: by tiles of 128 rows (0), by streams
+// of up to 16 or 32 (1, 2).
+template <typename DT, int HD, int SH, int OWN>
 __global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attention(PagedAttnArgs a) {
-  constexpr int TILE_BYTES = QS ? (int)sizeof(typename TileShape<HD>::Lds) : 0, STREAM_BYTES = RT ? StreamShape<DT, HD>::LDS * (int)sizeof(float) : 0;
+  constexpr bool TILES = SH == 1 || SH == 2 || OWN == 0, STREAMS = OWN > 0;
+  constexpr int TILE_BYTES = TILES ? (int)sizeof(typename TileShape<HD>::Lds) : 0, STREAM_BYTES = STREAMS ? StreamShape<DT, HD>::LDS * (int)sizeof(float) : 0;
   __shared__ __align__(16) unsigned char lds[TILE_BYTES > STREAM_BYTES ? TILE_BYTES : STREAM_BYTES];
-  const int id = blockIdx.x;
-  if constexpr (QS > 0) {
-    if (RT == 0 || id < a.tile_wgs) {
-      paged_tiles<HD, QS>(a, id, *(typename TileShape<HD>::Lds*)lds);
+  int id = blockIdx.x;
+  if constexpr (SH > 0) {
+    const int n = a.sh_slots * a.P_sh * a.p.nkv;
+    if (id < n) {
+      if constexpr (SH == 3) paged_stream<DT, HD, OWN, true>(a, id, (float*)lds);
+      else paged_tiles<HD, SH, true>(a, id, *(typename TileShape<HD>::Lds*)lds);
       return;
     }
+    id -= n;
   }
-  if constexpr (RT > 0) paged_stream<DT, HD, RT>(a, id - a.tile_wgs, (float*)lds);
+  if constexpr (OWN == 0) paged_tiles<HD, 1, false>(a, id, *(typename TileShape<HD>::Lds*)lds);
+  else paged_stream<DT, HD, OWN, false>(a, id, (float*)lds);
 }
 
 // Rows that have several parts, one wave per row and head: a lane has four dims of every STEP-th part, and all loads go out at once; the parts' factors go from lane

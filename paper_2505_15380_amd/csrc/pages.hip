@@ -105,34 +105,34 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
 // ------------------------------------------------------------------------------------------------ attention
 // How a call is cut.  From sizes that the caller gives alone, so that the workspace's size is known without a device.
 struct AttnCut {
-  int qs, rt;                                              // 128 qs packed rows of a workgroup of paged_tiles, 16 rt of one of paged_stream; 0: none
-  bool in_line, own_tiles;
+  int sh, own;                                             // k_paged_attention's SH and OWN
+  bool in_line, by_length;
   int P, P_sh, sh_chunks, own_chunks, sh_slots, own_slots;
 };
 static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, int n_rows, int max_len, int shared_positions) {
   constexpr int MAX_PARTS = 32;                            // of a source: 64 of a row
   AttnCut c;
   const bool b16 = dtype == SSD_DTYPE_BF16;
-  const int packed = n_rows * group, each = cdiv(packed, n_seqs), max_rt = hd == 128 ? 2 : 3;
+  const int packed = n_rows * group, each = cdiv(packed, n_seqs);
   c.in_line = n_seqs == 1 || each >= 256;
   const bool apart = shared_positions > 0 && !c.in_line;
-  c.own_tiles = b16 && each >= 48;
-  const bool sh_tiles = b16 && apart && packed >= 48;
-  c.qs = !c.own_tiles && !sh_tiles ? 0 : hd < 128 && (c.own_tiles ? each : packed) >= 512 ? 2 : 1;
-  c.rt = c.own_tiles ? 0 : each <= 16 ? 1 : max_rt;
-  const int own_t = c.own_tiles ? 128 * c.qs : 16 * c.rt, sh_t = sh_tiles ? 128 * c.qs : 16 * c.rt;
+  c.own = b16 && each > 32 ? 0 : each <= 16 ? 1 : 2;
+  c.sh = !apart ? 0 : !b16 || packed <= 32 ? 3 : hd < 128 && packed >= 512 ? 2 : 1;
+  if (c.sh == 3 && c.own == 0) c.sh = 1;
+  const int own_t = c.own ? 16 * c.own : 128, sh_t = c.sh == 3 ? 16 * c.own : 128 * c.sh;
   // parts: as many as give every compute unit work, of no fewer than `least` chunks
   auto parts = [&](int slots, int keys, int wgs, int least) {
     return std::max(1, std::min({wgs / std::max(1, slots * nkv), cdiv(std::max(1, cdiv(keys, PA_CHUNK)), least), MAX_PARTS}));
   };
   c.own_slots = packed / own_t + n_seqs;
   c.sh_slots = apart ? cdiv(packed, sh_t) : 0;
-  const int own = std::max(1, max_len - (apart ? shared_positions : 0)), own_parts = parts(std::max(n_seqs, packed / own_t), own, c.own_tiles ? 512 : 1024, 4);
+  const int own = std::max(1, max_len - (apart ? shared_positions : 0)), own_parts = parts(std::max(n_seqs, packed / own_t), own, c.own ? 1024 : 512, 4);
   c.own_chunks = cdiv(cdiv(own, PA_CHUNK), own_parts);
+  c.by_length = c.own == 0 && own_parts == 1 && n_seqs <= 256;
   c.P_sh = c.sh_chunks = 0;
   if (apart) {
     const int chunks = cdiv(shared_positions, PA_CHUNK);
-    c.sh_chunks = cdiv(chunks, parts(c.sh_slots, shared_positions, sh_tiles ? 512 : 1024, 4));
+    c.sh_chunks = cdiv(chunks, parts(c.sh_slots, shared_positions, c.sh == 3 ? 1024 : 512, 4));
     c.P_sh = cdiv(chunks, c.sh_chunks);
   }
   c.P = c.P_sh + own_parts;
@@ -154,11 +154,11 @@ extern "C" size_t ssd_paged_attention_workspace_bytes(const ssd_pages* pages, in
   return attention_ws(cut_attention(pages->dtype, p.hd, p.nkv, n_q_heads / p.nkv, n_seqs, n_rows, max_len, shared_blocks * p.bt), n_rows, n_q_heads, p.hd);
 }
 
-template <typename DT, int HD, int QS, int RT>
+template <typename DT, int HD, int SH, int OWN>
 static int launch_attention(const PagedAttnArgs& a, hipStream_t st) {
   const long long wgs = ((long long)a.sh_slots * a.P_sh + (long long)a.own_slots * (a.P - a.P_sh)) * a.p.nkv;
   if (wgs > 0x7FFFFFFFll) return fail(SSD_ENOSUP, "too many workgroups");
-  hipLaunchKernelGGL((k_paged_attention<DT, HD, QS, RT>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
+  hipLaunchKernelGGL((k_paged_attention<DT, HD, SH, OWN>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
   LAUNCH_CHECK();
   if (a.P > 1) {
     hipLaunchKernelGGL((k_paged_attention_merge<DT, HD>), dim3((unsigned)cdiv(a.n_rows * a.nq, BLOCK / WAVE)), dim3(BLOCK), 0, st, a);
@@ -166,16 +166,22 @@ static int launch_attention(const PagedAttnArgs& a, hipStream_t st) {
   }
   return SSD_OK;
 }
+template <typename DT, int HD, int SH>
+static int launch_own(const PagedAttnArgs& a, int own, hipStream_t st) {
+  if constexpr (std::is_same<DT, BF16>::value && SH != 3)
+    if (own == 0) return launch_attention<DT, HD, SH, 0>(a, st);
+  return own == 1 ? launch_attention<DT, HD, SH, 1>(a, st) : launch_attention<DT, HD, SH, 2>(a, st);
+}
 template <typename DT, int HD>
 static int launch_paged_attention(const PagedAttnArgs& a, const AttnCut& c, hipStream_t st) {
-  constexpr int MANY = HD == 128 ? 2 : 3;
+  if (c.sh == 0) return launch_own<DT, HD, 0>(a, c.own, st);
+  if (c.sh == 3) return launch_own<DT, HD, 3>(a, c.own, st);
   if constexpr (std::is_same<DT, BF16>::value) {
-    if constexpr (HD < 128) {
-      if (c.qs == 2) return c.rt == 0 ? launch_attention<DT, HD, 2, 0>(a, st) : c.rt == 1 ? launch_attention<DT, HD, 2, 1>(a, st) : launch_attention<DT, HD, 2, MANY>(a, st);
-    }
-    if (c.qs == 1) return c.rt == 0 ? launch_attention<DT, HD, 1, 0>(a, st) : c.rt == 1 ? launch_attention<DT, HD, 1, 1>(a, st) : launch_attention<DT, HD, 1, MANY>(a, st);
+    if constexpr (HD < 128)
+      if (c.sh == 2) return launch_own<DT, HD, 2>(a, c.own, st);
+    return launch_own<DT, HD, 1>(a, c.own, st);
   }
-  return c.rt == 1 ? launch_attention<DT, HD, 0, 1>(a, st) : launch_attention<DT, HD, 0, MANY>(a, st);
+  return fail(SSD_ENOSUP, "no kernel");
 }
 
 extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float scale, int n_seqs, int n_rows, int max_len, const int32_t* dev_len,
@@ -201,8 +207,7 @@ extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float 
   a.scale2 = scale * 1.44269504088896340736f;
   a.nq = n_q_heads; a.n_seqs = n_seqs; a.n_rows = n_rows; a.cap = table_cap; a.shared_blocks = shared_blocks;
   a.in_line = c.in_line && shared_blocks > 0;
-  a.tile_wgs = c.qs ? c.sh_slots * c.P_sh * a.p.nkv + (c.own_tiles ? c.own_slots * (c.P - c.P_sh) * a.p.nkv : 0) : 0;
-  a.own_tiles = c.own_tiles;
+  a.by_length = c.by_length;
   a.P = c.P; a.P_sh = c.P_sh; a.sh_chunks = c.sh_chunks; a.own_chunks = c.own_chunks; a.sh_slots = c.sh_slots; a.own_slots = c.own_slots;
   hipStream_t st = (hipStream_t)stream;
   const bool b16 = pages->dtype == SSD_DTYPE_BF16;
