@@ -72,6 +72,9 @@ __device__ __forceinline__ SeqRows seq_rows(const PagedAttnArgs& a, int s) {
   return r;
 }
 
+// (what the compiler cannot see to be the same in all lanes it keeps in vector registers, and makes a mask of every condition on it)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // What a workgroup does: packed rows row0 .. of n_packed, whose first row is seq_r0, against keys k_begin .. k_end - 1.
 struct Work {
   const int32_t* table;
@@ -97,16 +100,16 @@ __device__ __forceinline__ bool shared_work(const PagedAttnArgs& a, int id, int 
 }
 // A tile of sequence s against a part of its keys.
 __device__ __forceinline__ void own_tile(const PagedAttnArgs& a, const SeqRows& r, int s, int row0, int part, int T, int G, Work& w) {
-  w.row0 = row0;
-  w.n_packed = r.n * G;
-  w.table = a.table + (size_t)s * a.cap;
+  w.row0 = uniform(row0);
+  w.n_packed = uniform(r.n * G);
+  w.table = a.table + (size_t)uniform(s) * a.cap;
   w.table_n = a.cap;
-  w.head = r.head;
-  w.seq_r0 = r.r0;
-  w.len = r.len;
-  w.k_begin = r.start + part * r.per * PA_CHUNK;
-  w.k_end = min(r.len + min(r.n - 1, (row0 + T - 1) / G) + 1, w.k_begin + r.per * PA_CHUNK);        // (up to the last position that a row of the tile sees)
-  w.slot = r.chunks <= r.per && r.start == 0 ? -1 : a.P_sh + part;
+  w.head = uniform(r.head);
+  w.seq_r0 = uniform(r.r0);
+  w.len = uniform(r.len);
+  w.k_begin = uniform(r.start + part * r.per * PA_CHUNK);
+  w.k_end = uniform(min(r.len + min(r.n - 1, (row0 + T - 1) / G) + 1, w.k_begin + r.per * PA_CHUNK));        // (up to the last position that a row of the tile sees)
+  w.slot = uniform(r.chunks <= r.per && r.start == 0 ? -1 : a.P_sh + part);
   w.shared = false;
 }
 __device__ __forceinline__ bool own_work(const PagedAttnArgs& a, int id, int T, int G, Work& w) {
@@ -141,7 +144,7 @@ __device__ __forceinline__ bool own_work_by_length(const PagedAttnArgs& a, int r
       const SeqRows r = seq_rows(a, s);
       n += tiles(r) - first_of(r, c);
     }
-    return (int)wave_sum((float)n);
+    return uniform((int)wave_sum((float)n));
   };
   int bad = 0, longest = 0;
   for (int s = lane; s < a.n_seqs; s += 64) {
@@ -150,7 +153,7 @@ __device__ __forceinline__ bool own_work_by_length(const PagedAttnArgs& a, int r
     longest = max(longest, r.ok ? r.chunks : 0);
   }
   if (rank == 0 && bad && a.status) atomicOr(a.status, ST_BAD);
-  int lo = 0, hi = (int)wave_max((float)longest) + 1;      // more than `rank` tiles have at least lo chunks (any have 0), no more than that have hi (fewer than 2^24: exact)
+  int lo = 0, hi = uniform((int)wave_max((float)longest)) + 1;      // more than `rank` tiles have at least lo chunks (any have 0), no more than that have hi (fewer than 2^24: exact)
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
     if (count(mid) > rank) lo = mid; else hi = mid;
@@ -419,7 +422,8 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
 
 // ---------------------------------------------------------------------------------------------- many rows: through LDS (bf16)
 // A workgroup takes 128 QS packed query rows, 32 QS a wave, and a part of the keys, whose 64-key chunks all of its waves read from LDS, where direct
-// loads put them a chunk ahead (wave w the 16 keys w of a chunk, which lie in one block).  32x32x16 products: a lane holds the scores of one row
+// loads put them a chunk ahead (wave w the 16 keys w of a chunk, which lie in one block).  With KW 2 it takes half the rows: two waves have the same ones, one the
+// first 32 keys of every chunk and one the others, and meet in LDS at the end.  (Verifications have few more than 32 rows: two of four waves would be idle.)  32x32x16 products: a lane holds the scores of one row
 // (lane % 32) for keys 16 (i / 8) + 8 h + i % 8 of a 32-key tile (i: register, h = lane / 32) if row m of the tile's operand is the key whose bits 2 and 3
 // are those of m swapped; these are the operand of the second product as they stand.
 //   A direct load brings 1 KB of consecutive memory where the layout has it, so keys are parked [group of 16][key][16-byte unit] and values [group of
@@ -431,9 +435,9 @@ struct TileShape {
   typedef u32x4 Lds[2][2][4][J][64];   // [buffer][keys, values][group][..]
 };
 
-template <int HD, int QS, bool SHARED>
+template <int HD, int QS, int KW, bool SHARED>
 __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, typename TileShape<HD>::Lds& kv_lds) {
-  constexpr int J = HD / 32, T = 128 * QS;
+  constexpr int J = HD / 32, T = 128 * QS / KW, NT = 2 / KW;         // NT: 32-key tiles of a chunk that a wave multiplies, from t0 on
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, h = lane >> 5;
   const int nkv = a.p.nkv, G = a.nq / nkv, kvh = id % nkv, tmask = a.p.bt - 1;
   id /= nkv;
@@ -441,7 +445,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
   if (!(SHARED ? shared_work(a, id, T, G, w) : a.by_length ? own_work_by_length(a, id, T, G, w) : own_work(a, id, T, G, w))) return;
   const int n_chunks = max(0, ceil_div(w.k_end - w.k_begin, PA_CHUNK));
   // this wave's rows and what they see
-  const int w0 = w.row0 + wave * 32 * QS;
+  const int w0 = w.row0 + wave % (4 / KW) * 32 * QS, t0 = KW == 2 ? wave >> 1 : 0;
   const bool has_rows = w0 < w.n_packed;
   const int reach = !has_rows ? -1 : w.shared ? 0x7FFFFFFF : w.len + (min(w0 + 32 * QS, w.n_packed) - 1) / G;
   const int full_to = min(w.k_end, w.shared ? 0x7FFFFFFF : w.len + w0 / G + 1);        // keys before this one are there for all of the wave's rows
@@ -505,6 +509,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
       for (int i = 0; i < 16; ++i) o[x][d][i] = 0.f;
   }
   if (n_chunks > 0) request(0);
+  bool first = true;                                       // (the same in all lanes)
   for (int it = 0; it < n_chunks; ++it) {
     const int kbase = w.k_begin + it * PA_CHUNK;
     const int now = (int)(have >> ((it & 15) * 4)) & 15;
@@ -536,40 +541,40 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
       }
       request(it + 1);
     }
-    if (kbase > reach) continue;
+    if (kbase + 32 * t0 > reach) continue;
     const bool edge = now != 15 || kbase + PA_CHUNK > full_to;
     // Weights by the references that the rows have; if some row's come out too large - the first chunk's always do - they are taken again, after a look at the
     // largest scores, from the keys, which are still at hand.
-    bf16x8 p[QS][4];
+    bf16x8 p[QS][2 * NT];
     float sum[QS];
     auto weigh = [&](auto look) {
-      f32x16 s[QS][2];
+      f32x16 s[QS][NT];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int x = 0; x < QS; ++x)
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[x][t][i] = 0.f;
-      bf16x8 kf[2 * J][2];
+      bf16x8 kf[2 * J][NT];
 #pragma unroll
       for (int k = 0; k < 2 * J; ++k)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          kf[k][t] = __builtin_bit_cast(bf16x8, (&kv_lds[it & 1][0][2 * t + (kk >> 4)][0][0])[(kk & 15) * UNITS + ((2 * k + h) ^ ((kk & 15) >> SW & (UNITS - 1)))]);
+        for (int t = 0; t < NT; ++t)
+          kf[k][t] = __builtin_bit_cast(bf16x8, (&kv_lds[it & 1][0][2 * (t0 + t) + (kk >> 4)][0][0])[(kk & 15) * UNITS + ((2 * k + h) ^ ((kk & 15) >> SW & (UNITS - 1)))]);
 #pragma unroll
       for (int k = 0; k < 2 * J; ++k)                      // (chains side by side, or each product waits for the one before)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int x = 0; x < QS; ++x) s[x][t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k][t], q[x][k], s[x][t], 0, 0, 0);
       if (edge) {
 #pragma unroll
         for (int x = 0; x < QS; ++x) {
           const int pos = w.shared ? 0x7FFFFFFF : w.len + row[x] - w.seq_r0;
-          const int last = min(pos, w.k_end - 1) - kbase - 8 * h;            // of this lane's keys, less 8 h
+          const int last = min(pos, w.k_end - 1) - kbase - 32 * t0 - 8 * h;  // of this lane's keys, less 8 h
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            int last_y = now >> y & 1 ? last : -1;
+          for (int y = 0; y < 2 * NT; ++y) {
+            int last_y = now >> (2 * t0 + y) & 1 ? last : -1;
             asm volatile("" : "+v"(last_y));                                 // (or the comparisons are made for every chunk)
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -582,7 +587,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
         for (int x = 0; x < QS; ++x) {
           float mx = s[x][0][0];
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
+          for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][t][i]);
           const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
@@ -601,7 +606,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
       for (int x = 0; x < QS; ++x) {
         sum[x] = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < 2 * NT; ++k) {
           u32x4 w4;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -616,19 +621,53 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
       }
       return __any(large) != 0;
     };
-    if (it == 0 || weigh(std::false_type())) weigh(std::true_type());
+    if (first || weigh(std::false_type())) weigh(std::true_type());
+    first = false;
 #pragma unroll
     for (int x = 0; x < QS; ++x) l[x] += sum[x];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < 2 * NT; ++k)
 #pragma unroll
       for (int d = 0; d < J; ++d) {
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, kv_lds[it & 1][1][k][d][2 * c + (h ^ (c >> 3 & 1))]);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, kv_lds[it & 1][1][2 * t0 + k][d][2 * c + (h ^ (c >> 3 & 1))]);
 #pragma unroll
         for (int x = 0; x < QS; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[x][k], o[x][d], 0, 0, 0);
       }
   }
   if (__any(bad) && lane == 0 && a.status) atomicOr(a.status, ST_PAGE);
+  if constexpr (KW == 2) {
+    // the second wave's references, sums and outputs: [wave][QS][4 J + 1][lane] of four
+    static_assert(2 * QS * (4 * J + 1) * 64 <= 16 * J * 64, "");
+    f32x4* x4 = (f32x4*)&kv_lds[0][0][0][0][0] + (size_t)(wave & 1) * (QS * (4 * J + 1) * 64) + lane;
+    __syncthreads();                                       // (the last chunk has been read)
+    if (t0) {
+#pragma unroll
+      for (int x = 0; x < QS; ++x) {
+#pragma unroll
+        for (int d = 0; d < J; ++d)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x4[(x * (4 * J + 1) + d * 4 + e) * 64] = f32x4{o[x][d][4 * e], o[x][d][4 * e + 1], o[x][d][4 * e + 2], o[x][d][4 * e + 3]};
+        x4[(x * (4 * J + 1) + 4 * J) * 64] = f32x4{m[x], l[x], 0.f, 0.f};
+      }
+    }
+    __syncthreads();
+    if (t0) return;
+#pragma unroll
+    for (int x = 0; x < QS; ++x) {
+      const f32x4 ml = x4[(x * (4 * J + 1) + 4 * J) * 64];
+      const float mx = fmaxf(m[x], ml[0]), f0 = __builtin_amdgcn_exp2f(m[x] - mx), f1 = __builtin_amdgcn_exp2f(ml[0] - mx);
+      m[x] = mx;
+      l[x] = l[x] * f0 + ml[1] * f1;
+#pragma unroll
+      for (int d = 0; d < J; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 v = x4[(x * (4 * J + 1) + d * 4 + e) * 64];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[x][d][4 * e + i] = o[x][d][4 * e + i] * f0 + v[i] * f1;
+        }
+    }
+  }
 #pragma unroll
   for (int x = 0; x < QS; ++x) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[x]), __float_as_uint(l[x]), false, false);
@@ -656,10 +695,10 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
 }
 
 // The shared prefix first: its workgroups have the most to do.  SH: by tiles of 128 or 256 rows (1, 2), by streams (3), none (0); OWN: by tiles of 128 rows (0), by streams
-// of up to 16 or 32 (1, 2).
+// of up to 16 or 32 (1, 2), by tiles of 64 (3).
 template <typename DT, int HD, int SH, int OWN>
 __global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attention(PagedAttnArgs a) {
-  constexpr bool TILES = SH == 1 || SH == 2 || OWN == 0, STREAMS = OWN > 0;
+  constexpr bool STREAMS = OWN == 1 || OWN == 2, TILES = SH == 1 || SH == 2 || !STREAMS;
   constexpr int TILE_BYTES = TILES ? (int)sizeof(typename TileShape<HD>::Lds) : 0, STREAM_BYTES = STREAMS ? StreamShape<DT, HD>::LDS * (int)sizeof(float) : 0;
   __shared__ __align__(16) unsigned char lds[TILE_BYTES > STREAM_BYTES ? TILE_BYTES : STREAM_BYTES];
   int id = blockIdx.x;
@@ -667,12 +706,13 @@ __global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attention(PagedAttnArgs
     const int n = a.sh_slots * a.P_sh * a.p.nkv;
     if (id < n) {
       if constexpr (SH == 3) paged_stream<DT, HD, OWN, true>(a, id, (float*)lds);
-      else paged_tiles<HD, SH, true>(a, id, *(typename TileShape<HD>::Lds*)lds);
+      else paged_tiles<HD, SH, 1, true>(a, id, *(typename TileShape<HD>::Lds*)lds);
       return;
     }
     id -= n;
   }
-  if constexpr (OWN == 0) paged_tiles<HD, 1, false>(a, id, *(typename TileShape<HD>::Lds*)lds);
+  if constexpr (OWN == 0) paged_tiles<HD, 1, 1, false>(a, id, *(typename TileShape<HD>::Lds*)lds);
+  else if constexpr (OWN == 3) paged_tiles<HD, 1, 2, false>(a, id, *(typename TileShape<HD>::Lds*)lds);
   else paged_stream<DT, HD, OWN, false>(a, id, (float*)lds);
 }
 

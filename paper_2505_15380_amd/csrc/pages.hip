@@ -116,19 +116,20 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
   const int packed = n_rows * group, each = cdiv(packed, n_seqs);
   c.in_line = n_seqs == 1 || each >= 256;
   const bool apart = shared_positions > 0 && !c.in_line;
-  c.own = b16 && each > 32 ? 0 : each <= 16 ? 1 : 2;
+  c.own = b16 && each > 64 ? 0 : b16 && each > 32 ? 3 : each <= 16 ? 1 : 2;
   c.sh = !apart ? 0 : !b16 || packed <= 32 ? 3 : hd < 128 && packed >= 512 ? 2 : 1;
-  if (c.sh == 3 && c.own == 0) c.sh = 1;
-  const int own_t = c.own ? 16 * c.own : 128, sh_t = c.sh == 3 ? 16 * c.own : 128 * c.sh;
+  if (c.sh == 3 && (c.own == 0 || c.own == 3)) c.sh = 1;
+  const bool own_tiles = c.own == 0 || c.own == 3;
+  const int own_t = c.own == 0 ? 128 : c.own == 3 ? 64 : 16 * c.own, sh_t = c.sh == 3 ? 16 * c.own : 128 * c.sh;
   // parts: as many as give every compute unit work, of no fewer than `least` chunks
   auto parts = [&](int slots, int keys, int wgs, int least) {
     return std::max(1, std::min({wgs / std::max(1, slots * nkv), cdiv(std::max(1, cdiv(keys, PA_CHUNK)), least), MAX_PARTS}));
   };
   c.own_slots = packed / own_t + n_seqs;
   c.sh_slots = apart ? cdiv(packed, sh_t) : 0;
-  const int own = std::max(1, max_len - (apart ? shared_positions : 0)), own_parts = parts(std::max(n_seqs, packed / own_t), own, c.own ? 1024 : 512, 4);
+  const int own = std::max(1, max_len - (apart ? shared_positions : 0)), own_parts = parts(std::max(n_seqs, packed / own_t), own, own_tiles ? 512 : 1024, 4);
   c.own_chunks = cdiv(cdiv(own, PA_CHUNK), own_parts);
-  c.by_length = c.own == 0 && own_parts == 1 && n_seqs <= 256;
+  c.by_length = c.own == 0 && own_parts == 1 && !apart && n_seqs <= 64;
   c.P_sh = c.sh_chunks = 0;
   if (apart) {
     const int chunks = cdiv(shared_positions, PA_CHUNK);
@@ -169,7 +170,7 @@ static int launch_attention(const PagedAttnArgs& a, hipStream_t st) {
 template <typename DT, int HD, int SH>
 static int launch_own(const PagedAttnArgs& a, int own, hipStream_t st) {
   if constexpr (std::is_same<DT, BF16>::value && SH != 3)
-    if (own == 0) return launch_attention<DT, HD, SH, 0>(a, st);
+    if (own == 0 || own == 3) return own == 0 ? launch_attention<DT, HD, SH, 0>(a, st) : launch_attention<DT, HD, SH, 3>(a, st);
   return own == 1 ? launch_attention<DT, HD, SH, 1>(a, st) : launch_attention<DT, HD, SH, 2>(a, st);
 }
 template <typename DT, int HD>
