@@ -23,7 +23,7 @@
 
 namespace ssd {
 
-constexpr int PA_WAVES = 4, PA_THREADS = PA_WAVES * WAVE;
+constexpr int PA_WAVES = 4, PA_THREADS = PA_WAVES * WAVE;        // of a workgroup of tiles; streams that are by themselves have twice as many
 constexpr int PA_CHUNK = 64;           // keys in which parts are counted
 constexpr float PA_LAZY = 8.0f, PA_LARGE = 256.0f;
 constexpr float PA_NONE = -3.0e38f;    // the reference of a row that has seen nothing
@@ -208,10 +208,10 @@ struct StreamShape {
   static constexpr int FIT = 512 / (HD * (int)sizeof(typename DT::T)), NT = FIT < 4 ? FIT : 4, STEP = 16 * NT;      // keys and values of a step take 64 registers, or 32
   static constexpr int KU = B16 ? HD / 32 : HD / 16;       // 16-byte units of a key, or of a query row, that a lane has
   static constexpr int VU = HD / 16, VT = B16 ? NT / 2 : NT;           // dim tiles; pairs of key tiles, or tiles, that a value operand spans
-  static constexpr int LDS = PA_WAVES * 16 * (HD + 4) + 2 * PA_WAVES * 16;         // floats
+  static constexpr int LDS = 4 * 16 * (HD + 4) + 2 * 4 * 16;                       // floats: what four waves have of 16 rows
 };
 
-template <typename DT, int HD, int RT, bool SHARED>
+template <typename DT, int HD, int RT, int W, bool SHARED>
 __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, float* lds) {
   typedef typename DT::T T;
   typedef StreamShape<DT, HD> S;
@@ -226,7 +226,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
   const int pos_lo = w.shared ? 0x7FFFFFFF : w.len + w.row0 / G;
   // block ids of the wave's next 64 / NT steps: lane NT i + t has that of tile t of step i
   int bad = 0;
-  auto key_of = [&](int step) { return w.k_begin + ((step + lane / NT) * PA_WAVES + wave) * STEP + lane % NT * 16; };
+  auto key_of = [&](int step) { return w.k_begin + ((step + lane / NT) * W + wave) * STEP + lane % NT * 16; };
   int ids = block_of(a, w, key_of(0));
   int pos[RT];
   u32x4 q[RT][KU];
@@ -282,20 +282,20 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
       for (int d = 0; d < VU; ++d) vf[t][d] = *(const u32x4*)(vp + (d * 16 + li) * a.p.bt);
     }
   };
-  const int n_steps = max(0, ceil_div(w.k_end - w.k_begin, STEP)), mine = (n_steps - wave + PA_WAVES - 1) / PA_WAVES;
+  const int n_steps = max(0, ceil_div(w.k_end - w.k_begin, STEP)), mine = (n_steps - wave + W - 1) / W;
   const int first_key = w.k_begin + wave * STEP;
   if (mine > 0) { load_keys(0, first_key); load_values(0, first_key); }
   constexpr int PER = 64 / NT;                             // steps of a wave whose ids are at hand
   unsigned long long have = __ballot(ids >= 0);
   for (int i = 0; i < mine; ++i) {
-    const int k0 = first_key + i * PA_WAVES * STEP;
+    const int k0 = first_key + i * W * STEP;
     const int there = (int)(have >> (i % PER * NT)) & ((1 << NT) - 1);
     const bool more = i + 1 < mine, refill = more && (i + 1) % PER == 0;
     if (refill) {                                          // (this step's blocks are in `there`, its loads on their way)
       ids = checked_block(a, w, block_of(a, w, key_of(i + 1)), key_of(i + 1), bad);
       have = __ballot(ids >= 0);
     }
-    const int base_next = (i + 1) % PER * NT, k_next = k0 + PA_WAVES * STEP;
+    const int base_next = (i + 1) % PER * NT, k_next = k0 + W * STEP;
     const bool edge = there != (1 << NT) - 1 || k0 + STEP > w.k_end || k0 + STEP - 1 > pos_lo;
     if (edge) {
 #pragma unroll
@@ -381,26 +381,42 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
   }
   if (__any(bad) && lane == 0 && a.status) atomicOr(a.status, ST_PAGE);
   float (*po)[16][HD + 4] = (float (*)[16][HD + 4])lds;
-  float (*pm)[16] = (float (*)[16])(lds + PA_WAVES * 16 * (HD + 4)), (*pl)[16] = pm + PA_WAVES;
+  float (*pm)[16] = (float (*)[16])(lds + 4 * 16 * (HD + 4)), (*pl)[16] = pm + 4;
 #pragma unroll
   for (int x = 0; x < RT; ++x) {
     if (16 * x >= rows) break;
     if (x) __syncthreads();
-    const float ls = sum_over_groups(l[x]);
+    float ls = sum_over_groups(l[x]);
+    auto leave = [&](int at) {
 #pragma unroll
-    for (int d = 0; d < VU; ++d) *(f32x4*)&po[wave][li][d * 16 + g * 4] = o[x][d];
-    if (g == 0) { pm[wave][li] = m[x]; pl[wave][li] = ls; }
+      for (int d = 0; d < VU; ++d) *(f32x4*)&po[at][li][d * 16 + g * 4] = o[x][d];
+      if (g == 0) { pm[at][li] = m[x]; pl[at][li] = ls; }
+    };
+    if constexpr (W == 8) {                                // the upper four waves' go to the lower four
+      if (wave >= 4) leave(wave - 4);
+      __syncthreads();
+      if (wave < 4) {
+        const float m1 = pm[wave][li], mx = fmaxf(m[x], m1), f0 = __builtin_amdgcn_exp2f(m[x] - mx), f1 = __builtin_amdgcn_exp2f(m1 - mx);
+        m[x] = mx;
+        ls = ls * f0 + pl[wave][li] * f1;
+#pragma unroll
+        for (int d = 0; d < VU; ++d) o[x][d] = o[x][d] * f0 + *(const f32x4*)&po[wave][li][d * 16 + g * 4] * f1;
+        leave(wave);                                       // (where it has read)
+      }
+    } else {
+      leave(wave);
+    }
     __syncthreads();
-    for (int i = tid; i < 16 * (HD / 4); i += PA_THREADS) {
+    for (int i = tid; i < 16 * (HD / 4); i += W * WAVE) {
       const int r = i / (HD / 4), d = (i - r * (HD / 4)) * 4;
       if (16 * x + r >= rows) break;
       float mx = pm[0][r];
 #pragma unroll
-      for (int y = 1; y < PA_WAVES; ++y) mx = fmaxf(mx, pm[y][r]);
+      for (int y = 1; y < 4; ++y) mx = fmaxf(mx, pm[y][r]);
       float sum = 0.f;
       f32x4 acc = {0, 0, 0, 0};
 #pragma unroll
-      for (int y = 0; y < PA_WAVES; ++y) {
+      for (int y = 0; y < 4; ++y) {
         const float f = __builtin_amdgcn_exp2f(pm[y][r] - mx);
         sum = fmaf(pl[y][r], f, sum);
         acc += *(const f32x4*)&po[y][r][d] * f;
@@ -696,16 +712,21 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
 
 // The shared prefix first: its workgroups have the most to do.  SH: by tiles of 128 or 256 rows (1, 2), by streams (3), none (0); OWN: by tiles of 128 rows (0), by streams
 // of up to 16 or 32 (1, 2), by tiles of 64 (3).
+template <int SH, int OWN>
+struct PagedShape {
+  static constexpr bool STREAMS = OWN == 1 || OWN == 2, TILES = SH == 1 || SH == 2 || !STREAMS;
+  static constexpr int W = TILES ? PA_WAVES : 8, THREADS = W * WAVE;
+};
 template <typename DT, int HD, int SH, int OWN>
-__global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attention(PagedAttnArgs a) {
-  constexpr bool STREAMS = OWN == 1 || OWN == 2, TILES = SH == 1 || SH == 2 || !STREAMS;
-  constexpr int TILE_BYTES = TILES ? (int)sizeof(typename TileShape<HD>::Lds) : 0, STREAM_BYTES = STREAMS ? StreamShape<DT, HD>::LDS * (int)sizeof(float) : 0;
+__global__ void __launch_bounds__((PagedShape<SH, OWN>::THREADS), 2) k_paged_attention(PagedAttnArgs a) {
+  typedef PagedShape<SH, OWN> S;
+  constexpr int TILE_BYTES = S::TILES ? (int)sizeof(typename TileShape<HD>::Lds) : 0, STREAM_BYTES = S::STREAMS ? StreamShape<DT, HD>::LDS * (int)sizeof(float) : 0;
   __shared__ __align__(16) unsigned char lds[TILE_BYTES > STREAM_BYTES ? TILE_BYTES : STREAM_BYTES];
   int id = blockIdx.x;
   if constexpr (SH > 0) {
     const int n = a.sh_slots * a.P_sh * a.p.nkv;
     if (id < n) {
-      if constexpr (SH == 3) paged_stream<DT, HD, OWN, true>(a, id, (float*)lds);
+      if constexpr (SH == 3) paged_stream<DT, HD, OWN, S::W, true>(a, id, (float*)lds);
       else paged_tiles<HD, SH, 1, true>(a, id, *(typename TileShape<HD>::Lds*)lds);
       return;
     }
@@ -713,7 +734,7 @@ __global__ void __launch_bounds__(PA_THREADS, 2) k_paged_attention(PagedAttnArgs
   }
   if constexpr (OWN == 0) paged_tiles<HD, 1, 1, false>(a, id, *(typename TileShape<HD>::Lds*)lds);
   else if constexpr (OWN == 3) paged_tiles<HD, 1, 2, false>(a, id, *(typename TileShape<HD>::Lds*)lds);
-  else paged_stream<DT, HD, OWN, false>(a, id, (float*)lds);
+  else paged_stream<DT, HD, OWN, S::W, false>(a, id, (float*)lds);
 }
 
 // Rows that have several parts, one wave per row and head: a lane has four dims of every STEP-th part, and all loads go out at once; the parts' factors go from lane

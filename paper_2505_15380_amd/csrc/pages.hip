@@ -114,28 +114,55 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
   AttnCut c;
   const bool b16 = dtype == SSD_DTYPE_BF16;
   const int packed = n_rows * group, each = cdiv(packed, n_seqs);
-  c.in_line = n_seqs == 1 || each >= 256;
-  const bool apart = shared_positions > 0 && !c.in_line;
   c.own = b16 && each > 64 ? 0 : b16 && each > 32 ? 3 : each <= 16 ? 1 : 2;
+  // A prefix is in line with every sequence's own keys where nobody shares it, where a sequence's rows fill tiles of their own, or where reading it again for each costs
+  // less than the merge that two sources ask for, 4 us.
+  c.in_line = n_seqs == 1 || each >= 256 ||
+              (c.own && c.own < 3 && max_len <= 1024 && std::max(shared_positions * 0.0012, (double)n_seqs * shared_positions * nkv * hd * (b16 ? 4 : 8) / 4e6) < 4.0);
+  const bool apart = shared_positions > 0 && !c.in_line;
   c.sh = !apart ? 0 : !b16 || packed <= 32 ? 3 : hd < 128 && packed >= 512 ? 2 : 1;
   if (c.sh == 3 && (c.own == 0 || c.own == 3)) c.sh = 1;
   const bool own_tiles = c.own == 0 || c.own == 3;
   const int own_t = c.own == 0 ? 128 : c.own == 3 ? 64 : 16 * c.own, sh_t = c.sh == 3 ? 16 * c.own : 128 * c.sh;
-  // parts: as many as give every compute unit work, of no fewer than `least` chunks
-  auto parts = [&](int slots, int keys, int wgs, int least) {
-    return std::max(1, std::min({wgs / std::max(1, slots * nkv), cdiv(std::max(1, cdiv(keys, PA_CHUNK)), least), MAX_PARTS}));
-  };
   c.own_slots = packed / own_t + n_seqs;
   c.sh_slots = apart ? cdiv(packed, sh_t) : 0;
-  const int own = std::max(1, max_len - (apart ? shared_positions : 0)), own_parts = parts(std::max(n_seqs, packed / own_t), own, own_tiles ? 512 : 1024, 4);
-  c.own_chunks = cdiv(cdiv(own, PA_CHUNK), own_parts);
-  c.by_length = c.own == 0 && own_parts == 1 && !apart && n_seqs <= 64;
-  c.P_sh = c.sh_chunks = 0;
-  if (apart) {
-    const int chunks = cdiv(shared_positions, PA_CHUNK);
-    c.sh_chunks = cdiv(chunks, parts(c.sh_slots, shared_positions, c.sh == 3 ? 1024 : 512, 4));
-    c.P_sh = cdiv(chunks, c.sh_chunks);
+  // Chunks of a part: those of the least estimated time.  A workgroup of streams takes 4.5 us and 0.6 for each chunk of a wave, and there is room for 1024 of four waves or 512 of eight.
+  // Of tiles, a chunk costs a workgroup of 128 rows `unit` us beside another one on its compute unit, and a workgroup three chunks for being one; 512 have
+  // room at a time.  More than one part costs a launch of 4 us, and each part's result is written and read again at 4.7 TB/s.
+  const int own_keys = std::max(1, max_len - (apart ? shared_positions : 0)), own_n = cdiv(own_keys, PA_CHUNK), sh_n = cdiv(shared_positions, PA_CHUNK);
+  const int own_tile_n = std::max(n_seqs, packed / own_t);
+  const double unit = hd == 128 ? 2.2 : hd == 64 ? 1.4 : 1.0, part_us = (double)n_rows * nkv * group * (hd + 2) * 8 / 4.7e6;
+  const int waves = own_tiles || c.sh == 1 || c.sh == 2 ? 4 : 8;
+  auto stream_chunks = [&](int tiles, int n, bool alone) {
+    double best = 1e30;
+    int pick = n;
+    for (int p = 1; p <= MAX_PARTS; ++p) {
+      const int size = cdiv(n, p), parts = cdiv(n, size);
+      const double us = (4.5 + 0.6 * cdiv(size, waves)) * std::max(1.0, (double)tiles * nkv * parts / (4096 / waves)) + (parts > 1 && alone ? 4.0 : 0.0) + parts * part_us;
+      if (us < best) { best = us; pick = size; }
+    }
+    return pick;
+  };
+  c.own_chunks = own_tiles ? 0 : stream_chunks(own_tile_n, own_n, !apart);
+  c.sh_chunks = !apart ? 0 : c.sh == 3 ? stream_chunks(c.sh_slots, sh_n, false) : 0;
+  if (own_tiles || c.sh == 1 || c.sh == 2) {
+    double best = 1e30;
+    int pick = 0;
+    for (int i = 0; i < 2 * MAX_PARTS; ++i) {              // (one size for both sources: what divides either of them)
+      const int n = std::max(4, cdiv(i & 1 ? sh_n : own_n, (i >> 1) + 1));
+      const int so = own_tiles ? std::min(n, own_n) : 0, po = so ? cdiv(own_n, so) : 0, ss = apart && c.sh != 3 ? std::min(n, sh_n) : 0, ps = ss ? cdiv(sh_n, ss) : 0;
+      if (po > MAX_PARTS || ps > MAX_PARTS) continue;
+      const double cost_s = c.sh == 2 ? 1.8 : 1.0, cost_o = c.own == 3 ? 0.6 : 1.0;
+      const double load = (double)ps * c.sh_slots * nkv * (ss * cost_s + 3) + (double)po * own_tile_n * nkv * (so * cost_o + 3);
+      const double us = unit * std::max({load / 512, ss * cost_s + 3, so * cost_o + 3}) + (po + ps > 1 ? 4 + (po + ps) * part_us : 0);
+      if (us < best) { best = us; pick = n; }
+    }
+    if (own_tiles) c.own_chunks = std::min(pick, own_n);
+    if (apart && c.sh != 3) c.sh_chunks = std::min(pick, sh_n);
   }
+  const int own_parts = cdiv(own_n, c.own_chunks);
+  c.P_sh = apart ? cdiv(sh_n, c.sh_chunks) : 0;
+  c.by_length = c.own == 0 && own_parts == 1 && !apart && n_seqs <= 64;
   c.P = c.P_sh + own_parts;
   return c;
 }
@@ -159,7 +186,7 @@ template <typename DT, int HD, int SH, int OWN>
 static int launch_attention(const PagedAttnArgs& a, hipStream_t st) {
   const long long wgs = ((long long)a.sh_slots * a.P_sh + (long long)a.own_slots * (a.P - a.P_sh)) * a.p.nkv;
   if (wgs > 0x7FFFFFFFll) return fail(SSD_ENOSUP, "too many workgroups");
-  hipLaunchKernelGGL((k_paged_attention<DT, HD, SH, OWN>), dim3((unsigned)wgs), dim3(PA_THREADS), 0, st, a);
+  hipLaunchKernelGGL((k_paged_attention<DT, HD, SH, OWN>), dim3((unsigned)wgs), dim3(PagedShape<SH, OWN>::THREADS), 0, st, a);
   LAUNCH_CHECK();
   if (a.P > 1) {
     hipLaunchKernelGGL((k_paged_attention_merge<DT, HD>), dim3((unsigned)cdiv(a.n_rows * a.nq, BLOCK / WAVE)), dim3(BLOCK), 0, st, a);
