@@ -206,7 +206,7 @@ struct RopeAppendArgs {
 };
 
 constexpr int RA_HEADS = 4;            // heads of a thread
-constexpr int RA_WINDOW = 64;          // rows of a workgroup that puts values
+constexpr int RA_WINDOW = 32;          // rows of a workgroup that puts values
 
 // 16 bytes of a row as floats, and back, rounded once.
 template <typename DT>
@@ -214,8 +214,7 @@ struct Unit;
 template <>
 struct Unit<BF16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ void get(const bf16_t* p, float (&x)[8]) {
-    const u32x4 v = *(const u32x4*)p;
+  static __device__ __forceinline__ void get(const u32x4 v, float (&x)[8]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) { x[2 * e] = __uint_as_float(v[e] << 16); x[2 * e + 1] = __uint_as_float(v[e] & 0xFFFF0000u); }
   }
@@ -226,14 +225,17 @@ struct Unit<BF16> {
 template <>
 struct Unit<F32> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ void get(const float* p, float (&x)[4]) { *(f32x4*)x = *(const f32x4*)p; }
+  static __device__ __forceinline__ void get(const u32x4 v, float (&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(v[e]);
+  }
   static __device__ __forceinline__ void put(float* p, const float (&x)[4]) { *(f32x4*)p = *(const f32x4*)x; }
 };
 
 // The first `v_wgs` workgroups put values, the others turn queries and keys.
 //   Turning: a thread has 16 bytes of a row's first half of dims, the 16 of the second half that they are paired with, and their angles, for four
 // heads in turn.
-//   Values lie [dim][token], and a row brings one token of every dim: a workgroup takes 64 rows of a head through LDS and writes, for each dim, the
+//   Values lie [dim][token], and a row brings one token of every dim: a workgroup takes 32 rows of a head through LDS and writes, for each dim, the
 // eight tokens of an aligned piece at once (16 bytes; fp32 32) where eight rows behind each other fill one, the piece of a row being the business
 // of the workgroup that has its first row; what fills no piece goes element by element.
 template <typename DT>
@@ -246,21 +248,22 @@ __global__ void __launch_bounds__(BLOCK) k_rope_append(RopeAppendArgs a, int v_w
   const int hd = a.p.hd, tid = threadIdx.x;
   if ((int)blockIdx.x < v_wgs) {
     const int head = blockIdx.x % a.p.nkv, r0 = blockIdx.x / a.p.nkv * RA_WINDOW;
+    const int per = hd / N;
+    for (int i = tid; i < ROWS * per; i += BLOCK) {
+      const int r = i / per, u = i - r * per;
+      if (r0 + r < a.n_rows) *(u32x4*)&vals[r][u * N] = *(const u32x4*)((const T*)a.v + (size_t)(r0 + r) * a.v_stride + head * hd + u * N);
+    }
     if (tid < PIECE - 1 + ROWS) {
       const int r = r0 - (PIECE - 1) + tid;
       int s = -1;
       if (r >= 0 && r < a.n_rows) {
         s = a.row_slot[r];
+        const int pos = a.row_pos[r];
         const bool out = s >= 0 && (s >> a.p.bt_shift) >= a.p.n_blocks;
         if (out && a.status) atomicOr(a.status, ST_PAGE);
-        if (out || a.row_pos[r] < 0 || (a.rope && a.row_pos[r] >= a.positions)) s = -1;
+        if (out || pos < 0 || (a.rope && pos >= a.positions)) s = -1;
       }
       slots[tid] = s;
-    }
-    const int per = hd / N;
-    for (int i = tid; i < ROWS * per; i += BLOCK) {
-      const int r = i / per, u = i - r * per;
-      if (r0 + r < a.n_rows) *(u32x4*)&vals[r][u * N] = *(const u32x4*)((const T*)a.v + (size_t)(r0 + r) * a.v_stride + head * hd + u * N);
     }
     __syncthreads();
     if (tid < ROWS) {
@@ -315,24 +318,31 @@ __global__ void __launch_bounds__(BLOCK) k_rope_append(RopeAppendArgs a, int v_w
       c[2 * e] = v[0]; s[2 * e] = v[1]; c[2 * e + 1] = v[2]; s[2 * e + 1] = v[3];
     }
   }
+  u32x4 lo[RA_HEADS], hi[RA_HEADS];                        // (all of them requested at once)
+#pragma unroll
+  for (int k = 0; k < RA_HEADS; ++k) {
+    const int h = min(group * RA_HEADS + k, heads - 1);
+    const T* src = (h < a.nq ? (const T*)a.q + row * a.q_stride + h * hd : (const T*)a.k + row * a.k_stride + (h - a.nq) * hd) + d;
+    lo[k] = *(const u32x4*)src;
+    hi[k] = *(const u32x4*)(src + half);
+  }
 #pragma unroll
   for (int k = 0; k < RA_HEADS; ++k) {
     const int h = group * RA_HEADS + k;
     const bool is_q = h < a.nq;
     if (h >= heads || (!is_q && slot < 0)) break;
-    const T* src = is_q ? (const T*)a.q + row * a.q_stride + h * hd : (const T*)a.k + row * a.k_stride + (h - a.nq) * hd;
-    T* dst = is_q ? (T*)a.q_out + row * a.q_out_stride + h * hd
-                  : (T*)a.p.keys + (((size_t)(slot >> a.p.bt_shift) * a.p.nkv + (h - a.nq)) * a.p.bt + (slot & (a.p.bt - 1))) * hd;
+    T* dst = (is_q ? (T*)a.q_out + row * a.q_out_stride + h * hd
+                   : (T*)a.p.keys + (((size_t)(slot >> a.p.bt_shift) * a.p.nkv + (h - a.nq)) * a.p.bt + (slot & (a.p.bt - 1))) * hd) + d;
     float x[N], y[N], u[N], w[N];
-    Unit<DT>::get(src + d, x);
-    Unit<DT>::get(src + d + half, y);
+    Unit<DT>::get(lo[k], x);
+    Unit<DT>::get(hi[k], y);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       u[e] = x[e] * c[e] - y[e] * s[e];
       w[e] = y[e] * c[e] + x[e] * s[e];
     }
-    Unit<DT>::put(dst + d, u);
-    Unit<DT>::put(dst + d + half, w);
+    Unit<DT>::put(dst, u);
+    Unit<DT>::put(dst + half, w);
   }
 }
 
