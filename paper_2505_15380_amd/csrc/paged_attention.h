@@ -119,7 +119,7 @@ __device__ __forceinline__ bool own_work(const PagedAttnArgs& a, int id, int T, 
   const SeqRows r = seq_rows(a, s);
   w.row0 = (slot - (r.r0 * G / T + s)) * T;
   w.n_packed = r.n * G;
-  if (w.row0 >= w.n_packed) return false;
+  if (w.row0 < 0 || w.row0 >= w.n_packed) return false;    // (a first sequence that does not begin at row 0; an unused tile)
   if (!r.ok) {
     if (threadIdx.x == 0 && a.status) atomicOr(a.status, ST_BAD);
     return false;
@@ -195,6 +195,59 @@ __device__ __forceinline__ int checked_block(const PagedAttnArgs& a, const Work&
 // key's score stays -inf).
 __device__ __forceinline__ float factor(const PagedAttnArgs& a) { return a.scale2 == 0.f ? 1.f : fabsf(a.scale2); }
 __device__ __forceinline__ u32x4 factor_into(const PagedAttnArgs& a, u32x4 q, uint32_t signs) { return a.scale2 == 0.f ? u32x4{0, 0, 0, 0} : q ^ signs; }
+
+// Rows that share a tile do not all see its last keys.  The weight of a hidden key is 0, and 0 times a value that is not finite is NaN, so a row with such a key and a result
+// that is not finite is done over, by one wave, from the keys that it sees: the products then need no look at the values, and this is as rare as infinities in a cache are.
+__device__ __forceinline__ bool has_hidden(const Work& w, int G, int pr) { return !w.shared && w.len + pr / G + 1 < w.k_end; }
+__device__ __forceinline__ bool all_finite(f32x4 v) { return v[0] * 0.f + v[1] * 0.f + v[2] * 0.f + v[3] * 0.f == 0.f; }
+template <typename DT, int HD>
+__device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, int kvh, int G, int pr) {
+  typedef typename DT::T T;
+  constexpr int D = HD < 64 ? 1 : HD / 64;
+  const int lane = threadIdx.x & 63, dim = lane & (HD - 1), row = w.seq_r0 + pr / G, head = kvh * G + pr % G, end = min(w.len + pr / G + 1, w.k_end), tmask = a.p.bt - 1;
+  const T* q = (const T*)a.q + (size_t)row * a.q_stride + head * HD;
+  float acc[D] = {}, mx = PA_NONE, sum = 0.f;
+  for (int k0 = w.k_begin; k0 < end; k0 += 64) {
+    const int key = k0 + lane;
+    int bad = 0;
+    const int blk = key < end ? checked_block(a, w, block_of(a, w, key), key, bad) : -1;
+    float s = -INFINITY;
+    if (blk >= 0) {
+      const T* kp = (const T*)a.p.keys + (((size_t)blk * a.p.nkv + kvh) * a.p.bt + (key & tmask)) * HD;
+      float dot = 0.f;
+#pragma unroll 1
+      for (int d = 0; d < HD; ++d) dot = fmaf(DT::ld(q + d), DT::ld(kp + d), dot);
+      s = a.scale2 == 0.f ? 0.f : dot * a.scale2;
+    }
+    const float m = wave_max(s);
+    if (m > mx) {
+      const float keep = __builtin_amdgcn_exp2f(mx - m);
+      mx = m;
+      sum *= keep;
+#pragma unroll
+      for (int j = 0; j < D; ++j) acc[j] *= keep;
+    }
+    const float weight = __builtin_amdgcn_exp2f(s - mx);
+    sum += wave_sum(weight);
+#pragma unroll 1
+    for (int i = 0; i < min(64, end - k0); ++i) {
+      const int b = __builtin_amdgcn_readlane(blk, i);
+      if (b < 0) continue;
+      const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), i));
+      const T* vp = (const T*)a.p.values + (((size_t)b * a.p.nkv + kvh) * HD + dim) * a.p.bt + ((k0 + i) & tmask);
+#pragma unroll
+      for (int j = 0; j < D; ++j) acc[j] = fmaf(f, DT::ld(vp + 64 * j * a.p.bt), acc[j]);
+    }
+  }
+  const size_t at = ((size_t)row * a.nq + head) * a.P + w.slot;
+#pragma unroll
+  for (int j = 0; j < D; ++j) {
+    if (lane >= HD) continue;
+    if (w.slot < 0) DT::st((T*)a.out + (size_t)row * a.out_stride + head * HD + dim + 64 * j, sum == 0.f ? 0.f : acc[j] / sum);
+    else a.o_part[at * HD + dim + 64 * j] = acc[j];
+  }
+  if (w.slot >= 0 && lane == 0) { a.ml_part[at * 2] = mx; a.ml_part[at * 2 + 1] = sum; }
+}
 
 // ---------------------------------------------------------------------------------------------- few rows: from the pages into registers
 //   bf16  16x16x32 products.  Of a pair of 16-key tiles, row m of tile t is key 8 (m / 4) + 4 t + m % 4: lane group g = lane / 16 then ends with the scores of
@@ -380,6 +433,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
     if (more) load_values(base_next, k_next);
   }
   if (__any(bad) && lane == 0 && a.status) atomicOr(a.status, ST_PAGE);
+  uint32_t again = 0;                                      // rows of which this lane has written something that is not finite
   float (*po)[16][HD + 4] = (float (*)[16][HD + 4])lds;
   float (*pm)[16] = (float (*)[16])(lds + 4 * 16 * (HD + 4)), (*pl)[16] = pm + 4;
 #pragma unroll
@@ -422,6 +476,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
         acc += *(const f32x4*)&po[y][r][d] * f;
       }
       const int pr = w.row0 + 16 * x + r, row = w.seq_r0 + pr / G, head = kvh * G + pr % G;
+      if (!SHARED && !all_finite(acc)) again |= 1u << (16 * x + r);
       if (w.slot < 0) {
         T* dst = (T*)a.out + (size_t)row * a.out_stride + head * HD + d;
         acc *= sum == 0.f ? 0.f : 1.f / sum;
@@ -433,6 +488,12 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
         if (d == 0) { a.ml_part[at * 2] = mx; a.ml_part[at * 2 + 1] = sum; }
       }
     }
+  }
+  if (!SHARED && __any(again)) {
+    // (one wave has written the whole of a row; it writes it again behind that)
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    for (int r = 0; r < rows; ++r)
+      if (__any(again >> r & 1) && has_hidden(w, G, w.row0 + r)) redo_row<DT, HD>(a, w, kvh, G, w.row0 + r);
   }
 }
 
@@ -684,10 +745,17 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
         }
     }
   }
+  unsigned long long again[QS];                            // lanes that have written something that is not finite
 #pragma unroll
   for (int x = 0; x < QS; ++x) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[x]), __float_as_uint(l[x]), false, false);
     const float ls = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    f32x4 any = {0, 0, 0, 0};
+#pragma unroll
+    for (int d = 0; d < J; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any += f32x4{o[x][d][4 * e], o[x][d][4 * e + 1], o[x][d][4 * e + 2], o[x][d][4 * e + 3]} * 0.f;
+    again[x] = __ballot(!SHARED && !all_finite(any));
     if (w0 + 32 * x + c >= w.n_packed) continue;
     // dims 32 d + 8 e + 4 h .. + 3 in registers 4 e ..
     if (w.slot < 0) {
@@ -706,6 +774,17 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
 #pragma unroll
         for (int e = 0; e < 4; ++e) *(f32x4*)(dst + 32 * d + 8 * e) = f32x4{o[x][d][4 * e], o[x][d][4 * e + 1], o[x][d][4 * e + 2], o[x][d][4 * e + 3]};
       if (h == 0) { a.ml_part[at * 2] = m[x]; a.ml_part[at * 2 + 1] = ls; }
+    }
+  }
+  if constexpr (!SHARED) {
+#pragma unroll
+    for (int x = 0; x < QS; ++x) {
+      if (!again[x]) continue;
+      __builtin_amdgcn_s_waitcnt(0x0070);
+      for (int r = 0; r < 32; ++r) {
+        const int pr = w0 + 32 * x + r;
+        if (((again[x] | again[x] >> 32) >> r & 1) && pr < w.n_packed && has_hidden(w, G, pr)) redo_row<BF16, HD>(a, w, kvh, G, pr);
+      }
     }
   }
 }

@@ -456,6 +456,47 @@ def test_attention_is_nan_where_it_sees_nan_and_nowhere_else():
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("seqs, sb, heads", [([(30, 5), (90, 3), (0, 1)], 0, (6, 2, 64)), ([(40, 70), (0, 131)], 0, (12, 2, 128)), ([(200, 9), (3, 2)] * 8, 6, (14, 2, 64)),
+                                             ([(2000, 2), (3, 2)], 0, (4, 4, 32)), ([(62, 4), (0, 600)], 0, (2, 1, 64)), ([(900, 6)] * 3, 0, (8, 2, 64)), ([(61, 4), (127, 20)], 3, (4, 4, 32))])
+def test_attention_of_rows_before_values_that_are_not_finite(dtype, seqs, sb, heads):
+    """Infinities and NaN at new rows' positions are nothing to the rows before them, and come out at those that see them."""
+    b = Batch(seqs, *heads, 16, dtype, seed=sb + len(seqs), shared_blocks=sb)
+    G = heads[0] // heads[1]
+    expect = torch.zeros((b.n, heads[0], heads[2]), dtype=torch.float64, device="cuda")
+    for s, (n, r) in enumerate(zip(b.lens, b.rows)):
+        if r < 2:
+            continue
+        put = {(r // 2, 3): math.inf, (r // 2, 5): math.nan, (r // 2, 8): -math.inf, (r // 2, 9): math.inf}
+        put.update({(r - 1, 9): -math.inf, (r - 1, 31): math.inf})                 # (of two rows, the same one)
+        for (row, d), x in put.items():
+            b.values[int(b.table[s, (n + row) // 16]), heads[1] - 1, d, (n + row) % 16] = x
+            expect[b.start[s] + row:b.start[s + 1], heads[0] - G:, d] += x
+    out = b.run().double()
+    plain = torch.where(expect == 0, out, 0)
+    assert bool(torch.isfinite(plain).all())
+    for s in range(len(b.rows)):
+        o, e = b.oracle(s, b.hd ** -0.5)
+        at = slice(b.start[s], b.start[s + 1])
+        assert bool((((out[at] - o).abs() <= e) | (expect[at] != 0)).all()), s
+    differs = torch.where(expect == 0, 0, out).nan_to_num(nan=1.0, posinf=2.0, neginf=3.0) != expect.nan_to_num(nan=1.0, posinf=2.0, neginf=3.0)
+    assert not bool(differs.any())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("seqs, sb, heads", [([(30, 2), (90, 1), (700, 3)], 0, (6, 2, 64)), ([(20, 70), (900, 90)], 4, (4, 2, 64)), ([(3, 1)] * 70, 2, (4, 4, 32))])
+def test_attention_of_rows_that_begin_behind_others(dtype, seqs, sb, heads):
+    """The first sequence's rows need not be the first rows."""
+    b = Batch(seqs, *heads, 16, dtype, seed=11 + sb, shared_blocks=sb, pad=2)
+    b.q = torch.cat([torch.full_like(b.q[:19], math.nan), b.q])
+    b.start = [x + 19 for x in b.start]
+    out = torch.full_like(b.q, 7.0)
+    b.run(out=out)
+    assert b.status == 0
+    b.check(out)
+    assert bool((out[:19] == 7.0).all()) and bool((out[19 + b.n:] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 def test_attention_over_a_pool_of_more_than_2_31_elements(dtype):
     """Blocks far apart in a pool whose offsets take more than 32 bits of elements."""
     n_blocks = (1 << 31) // (2 * 16 * 128) + 1000
