@@ -55,13 +55,14 @@ def test_rope_append_refuses(lib, change, code):
 
 ATTEND = dict(pages=None, nq=4, scale=0.125, n_seqs=2, n_rows=3, max_len=100, len=P, row_start=P, table=P, cap=8, shared_blocks=1, shared_table=P, shared=None, q=P, qs=256, out=P,
               os=256, ws=P, ws_bytes=1 << 30, status=None, stream=None)
+LONG = dict(max_len=16000, cap=1000)                                           # keys that are read in parts: that takes a workspace
 
 
 @pytest.mark.parametrize("change, code", [
     (dict(nq=3), EINVAL), (dict(nq=0), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(n_seqs=0), EINVAL), (dict(n_seqs=(1 << 16) + 1), EINVAL),
     (dict(n_rows=-1), EINVAL), (dict(n_rows=(1 << 24) + 1), ENOSUP), (dict(max_len=0), EINVAL), (dict(len=None), EINVAL), (dict(row_start=None), EINVAL), (dict(table=None), EINVAL),
     (dict(shared_table=None), EINVAL), (dict(shared_blocks=-1), EINVAL), (dict(cap=0), EINVAL), (dict(cap=(1 << 26) + 1), EINVAL), (dict(q=None), EINVAL), (dict(out=None), EINVAL),
-    (dict(qs=100), EINVAL), (dict(os=258), EINVAL), (dict(ws=None), EINVAL), (dict(ws=P + 4), EINVAL), (dict(ws_bytes=0), ENOMEM),
+    (dict(qs=100), EINVAL), (dict(os=258), EINVAL), (dict(ws=None, **LONG), EINVAL), (dict(ws=P + 4, **LONG), EINVAL), (dict(ws_bytes=0, **LONG), ENOMEM),
 ])
 def test_paged_attention_refuses(lib, change, code):
     pg = pages()
