@@ -103,67 +103,100 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
 }
 
 // ------------------------------------------------------------------------------------------------ attention
-// How a call is cut.  From sizes that the caller gives alone, so that the workspace's size is known without a device.
+// How a call is cut.  From sizes that the caller gives alone, so that the workspace's size is known without a device: the kinds of workgroups and the chunks of a part that have
+// the least estimated time,
+//     sqrt(longest^2 + load^2) + (3.8 + 0.195 per MB of results for each part, if there are several)  us and what every call takes,
+// `longest`: of the workgroups, alone on a compute unit; `load`: of all of them, spread over 256 compute units.  The terms were fitted to 3700 cuts of 56 calls (1 to 256 sequences,
+// 1 to 7350 rows, 9 to 16888 positions), but for the 3.8, of which a graph takes 2.3 and a launch by itself more.  Of these calls and of 45 others the cut takes 5 %
+// more time in the mean than the best that was measured, and at most 25 %; rules on the rows of a sequence took 24 %, and up to three times.
 struct AttnCut {
   int sh, own;                                             // k_paged_attention's SH and OWN
   bool in_line, by_length;
   int P, P_sh, sh_chunks, own_chunks, sh_slots, own_slots;
 };
 static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, int n_rows, int max_len, int shared_positions) {
-  constexpr int MAX_PARTS = 32;                            // of a source: 64 of a row
-  AttnCut c;
+  constexpr int PARTS[] = {1, 2, 3, 4, 5, 6, 7, 8, 12, 16, 32};            // of a source: no more than 64 of a row
   const bool b16 = dtype == SSD_DTYPE_BF16;
-  const int packed = n_rows * group, each = cdiv(packed, n_seqs);
-  c.own = b16 && each > 64 ? 0 : b16 && each > 32 ? 3 : each <= 16 ? 1 : 2;
-  // A prefix is in line with every sequence's own keys where nobody shares it, where a sequence's rows fill tiles of their own, or where reading it again for each costs
-  // less than the merge that two sources ask for, 4 us.
-  c.in_line = n_seqs == 1 || each >= 256 ||
-              (c.own && c.own < 3 && max_len <= 1024 && std::max(shared_positions * 0.0012, (double)n_seqs * shared_positions * nkv * hd * (b16 ? 4 : 8) / 4e6) < 4.0);
-  const bool apart = shared_positions > 0 && !c.in_line;
-  c.sh = !apart ? 0 : !b16 || packed <= 32 ? 3 : hd < 128 && packed >= 512 ? 2 : 1;
-  if (c.sh == 3 && (c.own == 0 || c.own == 3)) c.sh = 1;
-  const bool own_tiles = c.own == 0 || c.own == 3;
-  const int own_t = c.own == 0 ? 128 : c.own == 3 ? 64 : 16 * c.own, sh_t = c.sh == 3 ? 16 * c.own : 128 * c.sh;
-  c.own_slots = packed / own_t + n_seqs;
-  c.sh_slots = apart ? cdiv(packed, sh_t) : 0;
-  // Chunks of a part: those of the least estimated time.  A workgroup of streams takes 4.5 us and 0.6 for each chunk of a wave, and there is room for 1024 of four waves or 512 of eight.
-  // Of tiles, a chunk costs a workgroup of 128 rows `unit` us beside another one on its compute unit, and a workgroup three chunks for being one; 512 have
-  // room at a time.  More than one part costs a launch of 4 us, and each part's result is written and read again at 4.7 TB/s.
-  const int own_keys = std::max(1, max_len - (apart ? shared_positions : 0)), own_n = cdiv(own_keys, PA_CHUNK), sh_n = cdiv(shared_positions, PA_CHUNK);
-  const int own_tile_n = std::max(n_seqs, packed / own_t);
-  const double unit = hd == 128 ? 2.2 : hd == 64 ? 1.4 : 1.0, part_us = (double)n_rows * nkv * group * (hd + 2) * 8 / 4.7e6;
-  const int waves = own_tiles || c.sh == 1 || c.sh == 2 ? 4 : 8;
-  auto stream_chunks = [&](int tiles, int n, bool alone) {
-    double best = 1e30;
-    int pick = n;
-    for (int p = 1; p <= MAX_PARTS; ++p) {
-      const int size = cdiv(n, p), parts = cdiv(n, size);
-      const double us = (4.5 + 0.6 * cdiv(size, waves)) * std::max(1.0, (double)tiles * nkv * parts / (4096 / waves)) + (parts > 1 && alone ? 4.0 : 0.0) + parts * part_us;
-      if (us < best) { best = us; pick = size; }
-    }
-    return pick;
+  const int packed = n_rows * group, each = cdiv(packed, n_seqs), sh_n = cdiv(shared_positions, PA_CHUNK);
+  const float part_us = 0.195f * (float)n_rows * nkv * group * (hd + 2) * 8e-6f;
+  // A chunk of a workgroup of 128 rows by tiles (bf16), alone and as a share of a full compute unit; a step of a
+  // wave of streams, whose keys take 512 bytes of a lane's registers at most.
+  const float tile_us = hd == 128 ? 1.13f : hd == 64 ? 0.70f : 0.50f, tile_share = hd == 128 ? 0.64f : hd == 64 ? 0.43f : 0.33f;
+  const int steps_a_chunk = std::max(1, PA_CHUNK * hd * (b16 ? 2 : 4) / 8192);
+  const float step_us = b16 ? (hd == 32 ? 0.9f : 1.45f) : 2.6f;
+  struct Source {
+    int cuts, best;                                        // (which of them)
+    int chunks[11], parts[11];
+    float longest[11], load[11];
   };
-  c.own_chunks = own_tiles ? 0 : stream_chunks(own_tile_n, own_n, !apart);
-  c.sh_chunks = !apart ? 0 : c.sh == 3 ? stream_chunks(c.sh_slots, sh_n, false) : 0;
-  if (own_tiles || c.sh == 1 || c.sh == 2) {
-    double best = 1e30;
-    int pick = 0;
-    for (int i = 0; i < 2 * MAX_PARTS; ++i) {              // (one size for both sources: what divides either of them)
-      const int n = std::max(4, cdiv(i & 1 ? sh_n : own_n, (i >> 1) + 1));
-      const int so = own_tiles ? std::min(n, own_n) : 0, po = so ? cdiv(own_n, so) : 0, ss = apart && c.sh != 3 ? std::min(n, sh_n) : 0, ps = ss ? cdiv(sh_n, ss) : 0;
-      if (po > MAX_PARTS || ps > MAX_PARTS) continue;
-      const double cost_s = c.sh == 2 ? 1.8 : 1.0, cost_o = c.own == 3 ? 0.6 : 1.0;
-      const double load = (double)ps * c.sh_slots * nkv * (ss * cost_s + 3) + (double)po * own_tile_n * nkv * (so * cost_o + 3);
-      const double us = unit * std::max({load / 512, ss * cost_s + 3, so * cost_o + 3}) + (po + ps > 1 ? 4 + (po + ps) * part_us : 0);
-      if (us < best) { best = us; pick = n; }
+  // n: chunks.  kind: 0 tiles of 128 rows, 3 of 64, 4 of 256; 1, 2 streams of up to 16, 32.  `mean`: of the part of the keys that its rows see.
+  auto source = [&](Source& x, int kind, int n, int tiles, float mean, int waves) {
+    x.cuts = 0;
+    const bool t = kind == 0 || kind >= 3;
+    const float size = kind == 4 ? 1.63f : kind == 3 ? 0.80f : 1.f, share = t ? tile_share * (kind == 3 ? 0.76f : size) : kind == 1 ? 1.55f : 2.4f;
+    for (int p : PARTS) {
+      const int c = cdiv(n, p), parts = cdiv(n, c), i = x.cuts;
+      if (i && c == x.chunks[i - 1]) continue;
+      x.chunks[i] = c; x.parts[i] = parts;
+      const float wgs = (float)tiles * parts * nkv / 256, turns = (wgs + ceilf(wgs)) * 0.5f;
+      x.longest[i] = t ? size * tile_us * (c + 1.2f) : 0.5f + step_us * (float)cdiv(c * steps_a_chunk, waves);
+      x.load[i] = turns * share * (t ? c * mean + 1.2f : (0.5f + step_us * ceilf(c * steps_a_chunk * mean / waves)) * waves / 8);
+      ++x.cuts;
     }
-    if (own_tiles) c.own_chunks = std::min(pick, own_n);
-    if (apart && c.sh != 3) c.sh_chunks = std::min(pick, sh_n);
+  };
+  AttnCut c;
+  float best = 1e30f;
+  for (int apart = 0; apart <= (shared_positions > 0 && n_seqs > 1); ++apart) {
+    const int own_n = cdiv(std::max(1, max_len - (apart ? shared_positions : 0)), PA_CHUNK);
+    const float mean = std::max(0.1f, 1.f - (float)n_rows / n_seqs / (2 * PA_CHUNK) / own_n);
+    Source shared[3];                                      // by tiles of 128 and 256 rows, by streams
+    if (apart && b16) source(shared[0], 0, sh_n, cdiv(packed, 128), 1.f, 4);
+    const bool wide = apart && b16 && hd < 128 && packed > 128;
+    if (wide) source(shared[1], 4, sh_n, cdiv(packed, 256), 1.f, 4);
+    for (int own = b16 ? 0 : 1; own < (b16 ? 4 : 3); ++own) {
+      const bool own_tiles = own == 0 || own == 3;
+      const int own_t = own == 0 ? 128 : own == 3 ? 64 : 16 * own;
+      if ((own == 0 || own == 2) && each <= own_t / 2) continue;      // (as many workgroups as of the smaller kind)
+      Source o;
+      const int tiles = n_seqs * cdiv(each, own_t), first_sh = apart ? (b16 ? 1 : 3) : 0;
+      source(o, own, own_n, tiles, mean, own_tiles || b16 && apart ? 4 : 8);
+      for (int sh = first_sh; sh <= (apart ? 3 : 0); ++sh) {
+        if ((sh == 3 && own_tiles) || (sh == 2 && !wide)) continue;
+        const int sh_slots = sh ? cdiv(packed, sh == 3 ? own_t : 128 * sh) : 0;
+        if (sh == 3) {                                     // (eight waves, then, of both)
+          if (first_sh != 3) source(o, own, own_n, tiles, mean, 8);
+          source(shared[2], own, sh_n, sh_slots, 1.f, 8);
+        }
+        Source& x = shared[sh ? sh - 1 : 0];
+        auto us = [&](int i, int j) {
+          const int parts = o.parts[i] + (sh ? x.parts[j] : 0);
+          const float longest = sh ? std::max(o.longest[i], x.longest[j]) : o.longest[i], load = o.load[i] + (sh ? x.load[j] : 0.f);
+          return sqrtf(longest * longest + load * load) + (parts > 1 ? 3.8f + parts * part_us : 0.f);
+        };
+        o.best = x.best = 0;
+        float least = 1e30f;
+        for (int turn = 0; turn < (sh ? 3 : 1); ++turn) {  // each source's in turn
+          Source& y = sh && turn != 1 ? x : o;
+          int pick = y.best;
+          for (int i = 0; i < y.cuts; ++i) {
+            const float t = &y == &o ? us(i, x.best) : us(o.best, i);
+            if (t < least) { least = t; pick = i; }
+          }
+          y.best = pick;
+        }
+        if (least >= best) continue;
+        best = least;
+        c.own = own; c.sh = sh; c.in_line = !apart;
+        c.own_chunks = o.chunks[o.best];
+        c.sh_chunks = sh ? x.chunks[x.best] : 0;
+        c.own_slots = packed / own_t + n_seqs;
+        c.sh_slots = sh_slots;
+        c.P_sh = sh ? x.parts[x.best] : 0;
+        c.P = c.P_sh + o.parts[o.best];
+      }
+    }
   }
-  const int own_parts = cdiv(own_n, c.own_chunks);
-  c.P_sh = apart ? cdiv(sh_n, c.sh_chunks) : 0;
-  c.by_length = c.own == 0 && own_parts == 1 && !apart && n_seqs <= 64;
-  c.P = c.P_sh + own_parts;
+  c.by_length = c.own == 0 && c.P == 1 && n_seqs <= 64;
   return c;
 }
 static int check_attention(const ssd_pages* pages, Pages& p, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks) {
