@@ -106,12 +106,12 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
 // How a call is cut.  From sizes that the caller gives alone, so that the workspace's size is known without a device: the kinds of workgroups and the chunks of a part that have
 // the least estimated time,
 //     sqrt(longest^2 + load^2) + (3.8 + 0.195 per MB of results for each part, if there are several)  us and what every call takes,
-// `longest`: of the workgroups, alone on a compute unit; `load`: of all of them, spread over 256 compute units.  The terms were fitted to 3700 cuts of 56 calls (1 to 256 sequences,
-// 1 to 7350 rows, 9 to 16888 positions), but for the 3.8, of which a graph takes 2.3 and a launch by itself more.  Of these calls and of 45 others the cut takes 5 %
-// more time in the mean than the best that was measured, and at most 25 %; rules on the rows of a sequence took 24 %, and up to three times.
+// `longest`: of the workgroups, alone on a compute unit; `load`: of all of them, spread over 256 compute units.  The terms were fitted to 7100 cuts of 126 calls (1 to 256 sequences,
+// 1 to 7600 rows, 9 to 16888 positions), but for the 3.8, of which a graph takes 2.3 and a launch by itself more.  The cut that is picked takes 5 % more time
+// in the mean than the best that was measured, and at most 25 %; rules on the rows of a sequence took 24 %, and up to three times.
 struct AttnCut {
   int sh, own;                                             // k_paged_attention's SH and OWN
-  bool in_line, by_length;
+  bool in_line;
   int P, P_sh, sh_chunks, own_chunks, sh_slots, own_slots;
 };
 static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, int n_rows, int max_len, int shared_positions) {
@@ -121,9 +121,9 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
   const float part_us = 0.195f * (float)n_rows * nkv * group * (hd + 2) * 8e-6f;
   // A chunk of a workgroup of 128 rows by tiles (bf16), alone and as a share of a full compute unit; a step of a
   // wave of streams, whose keys take 512 bytes of a lane's registers at most.
-  const float tile_us = hd == 128 ? 1.13f : hd == 64 ? 0.70f : 0.50f, tile_share = hd == 128 ? 0.64f : hd == 64 ? 0.43f : 0.33f;
+  const float tile_us = hd == 128 ? 1.13f : hd == 64 ? 0.73f : 0.52f, tile_share = hd == 128 ? 0.60f : hd == 64 ? 0.39f : 0.30f;
   const int steps_a_chunk = std::max(1, PA_CHUNK * hd * (b16 ? 2 : 4) / 8192);
-  const float step_us = b16 ? (hd == 32 ? 0.9f : 1.45f) : 2.6f;
+  const float step_us = b16 ? (hd == 32 ? 0.9f : hd == 64 ? 1.5f : 1.68f) : 2.35f;
   struct Source {
     int cuts, best;                                        // (which of them)
     int chunks[11], parts[11];
@@ -133,14 +133,16 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
   auto source = [&](Source& x, int kind, int n, int tiles, float mean, int waves) {
     x.cuts = 0;
     const bool t = kind == 0 || kind >= 3;
-    const float size = kind == 4 ? 1.63f : kind == 3 ? 0.80f : 1.f, share = t ? tile_share * (kind == 3 ? 0.76f : size) : kind == 1 ? 1.55f : 2.4f;
+    const float size = kind == 4 ? 1.6f : kind == 3 ? 0.78f : 1.f;
+    const float share = t ? tile_share * (kind == 3 ? 0.81f : size) : kind == 1 ? 1.37f : 2.25f;
     for (int p : PARTS) {
       const int c = cdiv(n, p), parts = cdiv(n, c), i = x.cuts;
       if (i && c == x.chunks[i - 1]) continue;
       x.chunks[i] = c; x.parts[i] = parts;
+      const float seen = parts == 1 ? mean : 1.f;
       const float wgs = (float)tiles * parts * nkv / 256, turns = (wgs + ceilf(wgs)) * 0.5f;
-      x.longest[i] = t ? size * tile_us * (c + 1.2f) : 0.5f + step_us * (float)cdiv(c * steps_a_chunk, waves);
-      x.load[i] = turns * share * (t ? c * mean + 1.2f : (0.5f + step_us * ceilf(c * steps_a_chunk * mean / waves)) * waves / 8);
+      x.longest[i] = t ? size * tile_us * (c + 1.8f) : 0.9f + step_us * (float)cdiv(c * steps_a_chunk, waves);
+      x.load[i] = turns * share * (t ? c * seen + 1.8f : (0.9f + step_us * ceilf(c * steps_a_chunk * seen / waves)) * waves / 8);
       ++x.cuts;
     }
   };
@@ -196,7 +198,6 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
       }
     }
   }
-  c.by_length = c.own == 0 && c.P == 1 && n_seqs <= 64;
   return c;
 }
 static int check_attention(const ssd_pages* pages, Pages& p, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks) {
@@ -268,7 +269,6 @@ extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float 
   a.scale2 = scale * 1.44269504088896340736f;
   a.nq = n_q_heads; a.n_seqs = n_seqs; a.n_rows = n_rows; a.cap = table_cap; a.shared_blocks = shared_blocks;
   a.in_line = c.in_line && shared_blocks > 0;
-  a.by_length = c.by_length;
   a.P = c.P; a.P_sh = c.P_sh; a.sh_chunks = c.sh_chunks; a.own_chunks = c.own_chunks; a.sh_slots = c.sh_slots; a.own_slots = c.own_slots;
   hipStream_t st = (hipStream_t)stream;
   const bool b16 = pages->dtype == SSD_DTYPE_BF16;
