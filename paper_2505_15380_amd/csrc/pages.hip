@@ -121,7 +121,7 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
   const float part_us = 0.195f * (float)n_rows * nkv * group * (hd + 2) * 8e-6f;
   // A chunk of a workgroup of 128 rows by tiles (bf16), alone and as a share of a full compute unit; a step of a
   // wave of streams, whose keys take 512 bytes of a lane's registers at most.
-  const float tile_us = hd == 128 ? 1.13f : hd == 64 ? 0.73f : 0.52f, tile_share = hd == 128 ? 0.60f : hd == 64 ? 0.39f : 0.30f;
+  const float tile_us = hd == 128 ? 1.13f : hd == 64 ? 0.73f : 0.52f, tile_share = hd == 128 ? 0.60f : hd == 64 ? 0.44f : 0.33f;
   const int steps_a_chunk = std::max(1, PA_CHUNK * hd * (b16 ? 2 : 4) / 8192);
   const float step_us = b16 ? (hd == 32 ? 0.9f : hd == 64 ? 1.5f : 1.68f) : 2.35f;
   struct Source {
@@ -134,7 +134,7 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
     x.cuts = 0;
     const bool t = kind == 0 || kind >= 3;
     const float size = kind == 4 ? 1.6f : kind == 3 ? 0.78f : 1.f;
-    const float share = t ? tile_share * (kind == 3 ? 0.81f : size) : kind == 1 ? 1.37f : 2.25f;
+    const float share = t ? tile_share * (kind == 3 ? (hd == 128 ? 0.8f : 0.6f) : size) : kind == 1 ? 1.37f : 2.25f;
     for (int p : PARTS) {
       const int c = cdiv(n, p), parts = cdiv(n, c), i = x.cuts;
       if (i && c == x.chunks[i - 1]) continue;
