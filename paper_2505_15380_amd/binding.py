@@ -422,11 +422,12 @@ class Pages:
         self.c = _Pages(keys.data_ptr(), values.data_ptr(), nb, nkv, bt, hd, _PAGE_DTYPES[self.dtype])
         self.ref = C.byref(self.c)
 
-    def rows(self, name, t, heads):
-        """Row stride of [rows, heads, head_dim] whose rows are in one piece each."""
+    def rows(self, name, t, heads, n=None):
+        """Row stride of [rows, heads, head_dim] whose rows are in one piece each; n: how many rows, if that is given."""
         sh, st, hd = t.shape, t.stride(), self.head_dim
-        if t.dtype is not self.dtype or t.get_device() != self.dev or len(sh) != 3 or sh[1] != heads or sh[2] != hd or st[2] != 1 or (st[1] != hd and heads != 1):
-            raise SSDError(-1, f"{name} is [rows, {heads}, {hd}] of the pages' type and device, the heads of a row behind each other")
+        if t.dtype is not self.dtype or t.get_device() != self.dev or len(sh) != 3 or sh[1] != heads or sh[2] != hd or st[2] != 1 or (st[1] != hd and heads != 1) or \
+                (n is not None and sh[0] != n):
+            raise SSDError(-1, f"{name} is [{'rows' if n is None else n}, {heads}, {hd}] of the pages' type and device, the heads of a row behind each other")
         return st[0] if sh[0] > 1 else heads * hd
 
 
@@ -450,22 +451,21 @@ def ssd_block_tables(lens, rows, block_tokens, table, owned, free_stack, n_free,
 def ssd_rope_append(pages, row_pos, row_slot, k, v, q=None, rope=None, q_out=None, status=None):
     """Rotary embedding of q and k and the append of k and v.  k, v [rows, n_kv_heads, head_dim], q [rows, n_q_heads, head_dim] or None (columns of one
     QKV product will do), rope [positions, head_dim / 2, 2] fp32 or None, row_pos, row_slot [rows] int32.  Returns q_out."""
-    n, nkv, dev = len(k), pages.n_kv_heads, _device_is_current(pages.keys)
-    ks, vs = pages.rows("k", k, nkv), pages.rows("v", v, nkv)
-    nq = qs = os_ = 0
-    if len(v) != n:
-        raise SSDError(-1, "k and v have the same rows")
+    n, nkv, dev = k.shape[0], pages.n_kv_heads, _device_is_current(pages.keys)
+    ks, vs = pages.rows("k", k, nkv, n), pages.rows("v", v, nkv, n)
+    nq = qs = os_ = positions = 0
     if q is not None:
         nq = q.shape[1]
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        qs, os_ = pages.rows("q", q, nq), pages.rows("q_out", q_out, nq)
-        if len(q) != n or len(q_out) != n:
-            raise SSDError(-1, "q and q_out have the rows of k")
-    if rope is not None and (rope.dtype is not torch.float32 or rope.get_device() != dev or not rope.is_contiguous() or rope.shape[1:] != (pages.head_dim // 2, 2)):
-        raise SSDError(-1, "rope is [positions, head_dim / 2, 2] fp32 in one piece on the device of the pages")
+        qs, os_ = pages.rows("q", q, nq, n), pages.rows("q_out", q_out, nq, n)
+    if rope is not None:
+        sh = rope.shape
+        if rope.dtype is not torch.float32 or rope.get_device() != dev or not rope.is_contiguous() or len(sh) != 3 or sh[1] != pages.head_dim // 2 or sh[2] != 2:
+            raise SSDError(-1, "rope is [positions, head_dim / 2, 2] fp32 in one piece on the device of the pages")
+        positions = sh[0]
     _check(load_library().ssd_rope_append(
-        pages.ref, n, nq, None if q is None else q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, None if rope is None else rope.data_ptr(), 0 if rope is None else len(rope),
+        pages.ref, n, nq, None if q is None else q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, None if rope is None else rope.data_ptr(), positions,
         _int_array("row_pos", row_pos, dev, n), _int_array("row_slot", row_slot, dev, n), None if q is None else q_out.data_ptr(), os_,
         None if status is None else _int_array("status", status, dev, 1), _stream()))
     return q_out
@@ -480,9 +480,7 @@ def ssd_paged_attention(pages, q, lens, row_start, table, scale=None, shared_tab
     dev, a = _device_is_current(pages.keys), _int_array
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    elif len(out) != n:
-        raise SSDError(-1, "out has the rows of q")
-    qs, os_ = pages.rows("q", q, nq), pages.rows("out", out, nq)
+    qs, os_ = pages.rows("q", q, nq), pages.rows("out", out, nq, n)
     sb = 0 if shared_table is None else shared_table.numel()
     if max_len is None:
         max_len = cap * pages.block_tokens
