@@ -5,8 +5,8 @@
 // shared prefix is one attention of ALL rows of the batch against the same keys, and each sequence's own keys another; what a row gets of both is merged.
 //
 // Two ways of taking a source of keys, whose query rows - rows x the G query heads of a kv head, packed [row][head] - share them:
-//   paged_tiles   128 or 256 packed rows a workgroup, keys and values through LDS: the shared prefix, prompts
-//   paged_stream  up to 32 packed rows, keys and values straight into registers: a sequence's own keys while it decodes or verifies; fp32
+//   paged_tiles   64, 128 or 256 packed rows a workgroup, keys and values through LDS: the shared prefix, prompts, verifications (bf16)
+//   paged_stream  up to 32 packed rows, keys and values straight into registers: a sequence's own keys while it decodes; fp32
 // and one launch has workgroups of both, so that the products of the one run beside the loads of the other.
 //
 // Scores and outputs are computed transposed (S^T = K Q^T, O^T = V^T P^T): a lane holds scores and outputs of one query row, the weights go from the
@@ -14,7 +14,15 @@
 // Weights are powers of two of scores less a reference, the largest score of the first keys, which moves only to one that exceeds it by
 // PA_LAZY: most steps need neither a maximum across lanes nor a scaling of what is summed.  A weight is then at most 2^8, and as exact.
 // The bf16 kernels round the weights to bf16 for the second product (2^-9 of each on average, at random: the sum is off by about as much as the
-// output's own rounding); their sum is taken of the unrounded ones, in fp32.
+// output's own rounding).  Their sum is held in fp32: tiles take it of the rounded weights, by dot instructions, streams of the unrounded ones.
+//
+// What bounds a call (0.5B heads, 14 x 64 over 2, bf16, one MI355X; kernel times):
+//   few rows      the dependent steps - lengths, table, keys, scores, values, LDS - of which one token over 1024 positions takes 8.3 us; 16 x 7 rows over 256 to 4096 positions 11.5
+//                 us and 4.0 for the merge, where the bytes would take 3.1
+//   a prefix      of 16384 positions for 256 x 5 rows: 97 us, 780 TFLOP/s; the matrix units are busy for 35 % of that, the vector units (weights: a power of two, a product, half a
+//                 conversion and half a sum each) for 45 %, and two waves of a SIMD hardly overlap the one with the other
+//   prompts       seven of 100 to 2001 rows behind 1024 positions: 70 us, 630 TFLOP/s, 26 and 36 %: the same, and compute units with four workgroups
+//                 beside ones with three
 #pragma once
 #include <type_traits>
 
@@ -199,7 +207,9 @@ __device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, 
 //         keys 8 g .. 8 g + 7, whose values it holds as the second product's operand.
 //   fp32  16x16x4 products: lane group g ends with keys 4 g .. 4 g + 3 of a tile.
 // A workgroup has up to RT tiles of 16 rows; its waves take steps of 16 NT keys in turn, each with references, sums and outputs of its own, and meet in
-// LDS.  The next step's keys are requested when this one's have been multiplied, its values likewise.
+// LDS.  The next step's keys are requested when this one's have been multiplied, its values likewise.  Bound by the loads' latency, of which a wave has one step's in flight: where streams
+// are by themselves they have eight waves, and keys that eight waves take in two or three steps need no parts (one token over 1024 positions: 10.2 us, in parts with a merge 14.6).
+// Through LDS keys would be written and read once each: no other wave wants them.
 template <typename DT, int HD>
 struct StreamShape {
   static constexpr bool B16 = sizeof(typename DT::T) == 2;
@@ -445,7 +455,8 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
 // ---------------------------------------------------------------------------------------------- many rows: through LDS (bf16)
 // A workgroup takes 128 QS packed query rows, 32 QS a wave, and a part of the keys, whose 64-key chunks all of its waves read from LDS, where direct
 // loads put them a chunk ahead (wave w the 16 keys w of a chunk, which lie in one block).  With KW 2 it takes half the rows: two waves have the same ones, one the
-// first 32 keys of every chunk and one the others, and meet in LDS at the end.  (Verifications have few more than 32 rows: two of four waves would be idle.)  32x32x16 products: a lane holds the scores of one row
+// first 32 keys of every chunk and one the others, and meet in LDS at the end.  (Verifications have few more than 32 rows: two of four waves would be idle.  16 x 7 rows: 15.0 us, with
+// 128 15.5, by streams 16.4.)  32x32x16 products: a lane holds the scores of one row
 // (lane % 32) for keys 16 (i / 8) + 8 h + i % 8 of a 32-key tile (i: register, h = lane / 32) if row m of the tile's operand is the key whose bits 2 and 3
 // are those of m swapped; these are the operand of the second product as they stand.
 //   A direct load brings 1 KB of consecutive memory where the layout has it, so keys are parked [group of 16][key][16-byte unit] and values [group of
@@ -762,7 +773,8 @@ __global__ void __launch_bounds__((PagedShape<SH, OWN>::THREADS), 2) k_paged_att
 }
 
 // Rows that have several parts, one wave per row and head: a lane has four dims of every STEP-th part, and all loads go out at once; the parts' factors go from lane
-// to lane.  Ascending parts in each lane, then lane by lane in a fixed order.
+// to lane.  Ascending parts in each lane, then lane by lane in a fixed order.  4 us for being a launch; 256 x 5 rows in 8 parts, 38 MB, 11.6 us.  (The last part to arrive could
+// merge, but its release and acquire cost more, and the counters would have to be zeroed.)
 template <typename DT, int HD>
 __global__ void __launch_bounds__(BLOCK) k_paged_attention_merge(PagedAttnArgs a) {
   typedef typename DT::T T;
