@@ -255,7 +255,8 @@ extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float 
   if (n_rows == 0) return SSD_OK;
   if (!dev_len || !dev_row_start || !dev_table || (shared_blocks > 0 && !dev_shared_table)) return fail(SSD_EINVAL, "null argument");
   if (table_cap < 1 || (long long)table_cap * a.p.bt > (1 << 30)) return fail(SSD_EINVAL, "table_cap = %d", table_cap);
-  if (!std::isfinite(scale)) return fail(SSD_EINVAL, "scale is not finite");
+  const float scale2 = scale * 1.44269504088896340736f;
+  if (!std::isfinite(scale2)) return fail(SSD_EINVAL, "scale, or scale * log2(e), is not finite");
   if (int rc = check_rows("q", dev_q, q_stride, n_q_heads, a.p, pages->dtype)) return rc;
   if (int rc = check_rows("out", dev_out, out_stride, n_q_heads, a.p, pages->dtype)) return rc;
   const AttnCut c = cut_attention(pages->dtype, a.p.hd, a.p.nkv, n_q_heads / a.p.nkv, n_seqs, n_rows, max_len, shared_blocks * a.p.bt);
@@ -266,7 +267,7 @@ extern "C" int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float 
   a.len = dev_len; a.row_start = dev_row_start; a.table = dev_table; a.shared_table = dev_shared_table; a.shared = dev_shared; a.status = dev_status;
   a.o_part = (float*)dev_ws;
   a.ml_part = a.o_part + (size_t)n_rows * n_q_heads * c.P * a.p.hd;
-  a.scale2 = scale * 1.44269504088896340736f;
+  a.scale2 = scale2;
   a.nq = n_q_heads; a.n_seqs = n_seqs; a.n_rows = n_rows; a.cap = table_cap; a.shared_blocks = shared_blocks;
   a.in_line = c.in_line && shared_blocks > 0;
   a.P = c.P; a.P_sh = c.P_sh; a.sh_chunks = c.sh_chunks; a.own_chunks = c.own_chunks; a.sh_slots = c.sh_slots; a.own_slots = c.own_slots;

@@ -483,6 +483,26 @@ def test_attention_of_rows_before_values_that_are_not_finite(dtype, seqs, sb, he
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("seqs, sb, heads", [([(30, 5), (90, 3)], 0, (6, 2, 64)), ([(40, 70), (0, 131)], 0, (12, 2, 128)), ([(200, 9), (3, 2)] * 8, 6, (14, 2, 64)), ([(62, 4), (0, 600)], 0, (4, 4, 32))])
+def test_attention_of_rows_before_keys_that_are_not_finite(dtype, seqs, sb, heads):
+    """A key of NaN makes NaN of the rows that see it, in the heads that read it, and nothing of others."""
+    b = Batch(seqs, *heads, 16, dtype, seed=sb + 3 * len(seqs), shared_blocks=sb)
+    G = heads[0] // heads[1]
+    seen = torch.zeros((b.n, heads[0], 1), dtype=torch.bool, device="cuda")
+    for s, (n, r) in enumerate(zip(b.lens, b.rows)):
+        row = r // 2
+        b.keys[int(b.table[s, (n + row) // 16]), 0, (n + row) % 16] = math.nan
+        b.keys[int(b.table[s, (n + r - 1) // 16]), 0, (n + r - 1) % 16, 1:] = math.inf
+        seen[b.start[s] + row:b.start[s + 1], :G] = True
+    out = b.run().double()
+    assert bool((torch.isnan(out) == seen).all())
+    for s in range(len(b.rows)):
+        o, e = b.oracle(s, b.hd ** -0.5)
+        at = slice(b.start[s], b.start[s + 1])
+        assert bool((((out[at] - o).abs() <= e) | seen[at]).all()), s
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("seqs, sb, heads", [([(30, 2), (90, 1), (700, 3)], 0, (6, 2, 64)), ([(20, 70), (900, 90)], 4, (4, 2, 64)), ([(3, 1)] * 70, 2, (4, 4, 32))])
 def test_attention_of_rows_that_begin_behind_others(dtype, seqs, sb, heads):
     """The first sequence's rows need not be the first rows."""

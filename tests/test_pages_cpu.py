@@ -59,7 +59,7 @@ LONG = dict(max_len=16000, cap=1000)                                           #
 
 
 @pytest.mark.parametrize("change, code", [
-    (dict(nq=3), EINVAL), (dict(nq=0), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(n_seqs=0), EINVAL), (dict(n_seqs=(1 << 16) + 1), EINVAL),
+    (dict(nq=3), EINVAL), (dict(nq=0), EINVAL), (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(scale=3e38), EINVAL), (dict(n_seqs=0), EINVAL), (dict(n_seqs=(1 << 16) + 1), EINVAL),
     (dict(n_rows=-1), EINVAL), (dict(n_rows=(1 << 24) + 1), ENOSUP), (dict(max_len=0), EINVAL), (dict(len=None), EINVAL), (dict(row_start=None), EINVAL), (dict(table=None), EINVAL),
     (dict(shared_table=None), EINVAL), (dict(shared_blocks=-1), EINVAL), (dict(cap=0), EINVAL), (dict(cap=(1 << 26) + 1), EINVAL), (dict(q=None), EINVAL), (dict(out=None), EINVAL),
     (dict(qs=100), EINVAL), (dict(os=258), EINVAL), (dict(ws=None, **LONG), EINVAL), (dict(ws=P + 4, **LONG), EINVAL), (dict(ws_bytes=0, **LONG), ENOMEM),
