@@ -764,12 +764,12 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
   }
 }
 
-// The shared prefix first: its workgroups have the most to do.  SH: by tiles of 128 or 256 rows (1, 2), by streams (3), none (0); OWN: by tiles of 128 rows (0), by streams
-// of up to 16 or 32 (1, 2), by tiles of 64 (3).
+// The shared prefix first: its workgroups have the most to do.  SH: by tiles of 128 or 256 rows (1, 2), by streams (3), none (0); OWN: by tiles of 128 rows (0), by tiles of 64 (3), by streams of up to 16 (1);
+// fp32 by streams of up to 16 or 32 rows (1, 2), of four waves where there is no other source (4, 5).
 template <int SH, int OWN>
 struct PagedShape {
-  static constexpr bool STREAMS = OWN == 1 || OWN == 2, TILES = SH == 1 || SH == 2 || !STREAMS;
-  static constexpr int W = TILES ? PA_WAVES : 8, THREADS = W * WAVE;
+  static constexpr bool STREAMS = OWN != 0 && OWN != 3, TILES = SH == 1 || SH == 2 || !STREAMS;
+  static constexpr int RT = OWN > 3 ? OWN - 3 : OWN, W = TILES || OWN > 3 ? PA_WAVES : 8, THREADS = W * WAVE;
 };
 template <typename DT, int HD, int SH, int OWN>
 __global__ void __launch_bounds__((PagedShape<SH, OWN>::THREADS), 2) k_paged_attention(PagedAttnArgs a) {
@@ -780,7 +780,7 @@ __global__ void __launch_bounds__((PagedShape<SH, OWN>::THREADS), 2) k_paged_att
   if constexpr (SH > 0) {
     const int n = a.sh_slots * a.P_sh * a.p.nkv;
     if (id < n) {
-      if constexpr (SH == 3) paged_stream<DT, HD, OWN, S::W, true>(a, id, (float*)lds);
+      if constexpr (SH == 3) paged_stream<DT, HD, S::RT, S::W, true>(a, id, (float*)lds);
       else paged_tiles<HD, SH, 1, true>(a, id, *(typename TileShape<HD>::Lds*)lds);
       return;
     }
@@ -788,7 +788,7 @@ __global__ void __launch_bounds__((PagedShape<SH, OWN>::THREADS), 2) k_paged_att
   }
   if constexpr (OWN == 0) paged_tiles<HD, 1, 1, false>(a, id, *(typename TileShape<HD>::Lds*)lds);
   else if constexpr (OWN == 3) paged_tiles<HD, 1, 2, false>(a, id, *(typename TileShape<HD>::Lds*)lds);
-  else paged_stream<DT, HD, OWN, S::W, false>(a, id, (float*)lds);
+  else paged_stream<DT, HD, S::RT, S::W, false>(a, id, (float*)lds);
 }
 
 // Rows that have several parts, one wave per row and head: a lane has four dims of every STEP-th part, and all loads go out at once; the parts' factors go from lane

@@ -129,13 +129,17 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
     int chunks[11], parts[11];
     float longest[11], load[11];
   };
+  // bf16 pages have streams of up to 16 rows (more rows are faster by tiles), fp32 of up to 16 and 32, and those of four waves too: many sequences of few
+  // keys are done in fewer rounds of workgroups (243 of up to 335 positions 50.4 -> 31.0 us), few of many keys wait longer (4 behind 3904 positions 56.7, four
+  // waves 86.7), and parts are for eight (90 behind 5488 positions 59.2, in parts of four waves 79.1).
   // n: chunks.  kind: 0 tiles of 128 rows, 3 of 64, 4 of 256; 1, 2 streams of up to 16, 32.  `mean`: of the part of the keys that its rows see.
-  auto source = [&](Source& x, int kind, int n, int tiles, float mean, int waves) {
+  auto source = [&](Source& x, int kind, int n, int tiles, float mean, int waves, bool whole = false) {
     x.cuts = 0;
     const bool t = kind == 0 || kind >= 3;
     const float size = kind == 4 ? 1.6f : kind == 3 ? 0.78f : 1.f;
     const float share = t ? tile_share * (kind == 3 ? (hd == 128 ? 0.8f : 0.6f) : size) : kind == 1 ? 1.37f : 2.25f;
     for (int p : PARTS) {
+      if (whole && p > 1) break;
       const int c = cdiv(n, p), parts = cdiv(n, c), i = x.cuts;
       if (i && c == x.chunks[i - 1]) continue;
       x.chunks[i] = c; x.parts[i] = parts;
@@ -155,13 +159,14 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
     if (apart && b16) source(shared[0], 0, sh_n, cdiv(packed, 128), 1.f, 4);
     const bool wide = apart && b16 && hd < 128 && packed > 128;
     if (wide) source(shared[1], 4, sh_n, cdiv(packed, 256), 1.f, 4);
-    for (int own = b16 ? 0 : 1; own < (b16 ? 4 : 3); ++own) {
+    for (int own = b16 ? 0 : 1; own < (b16 ? 4 : 6); ++own) {
       const bool own_tiles = own == 0 || own == 3;
-      const int own_t = own == 0 ? 128 : own == 3 ? 64 : 16 * own;
-      if ((own == 0 || own == 2) && each <= own_t / 2) continue;      // (as many workgroups as of the smaller kind)
+      if (b16 ? own == 2 : own == 3 || (own > 3 && apart)) continue;
+      const int rt = own > 3 ? own - 3 : own, own_t = own == 0 ? 128 : own == 3 ? 64 : 16 * rt;
+      if ((own == 0 || rt == 2) && each <= own_t / 2) continue;       // (as many workgroups as of the smaller kind)
       Source o;
       const int tiles = n_seqs * cdiv(each, own_t), first_sh = apart ? (b16 ? 1 : 3) : 0;
-      source(o, own, own_n, tiles, mean, own_tiles || b16 && apart ? 4 : 8);
+      source(o, own_tiles ? own : rt, own_n, tiles, mean, own_tiles || (b16 && apart) || own > 3 ? 4 : 8, own > 3);
       for (int sh = first_sh; sh <= (apart ? 3 : 0); ++sh) {
         if ((sh == 3 && own_tiles) || (sh == 2 && !wide)) continue;
         const int sh_slots = sh ? cdiv(packed, sh == 3 ? own_t : 128 * sh) : 0;
@@ -230,9 +235,15 @@ static int launch_attention(const PagedAttnArgs& a, hipStream_t st) {
 }
 template <typename DT, int HD, int SH>
 static int launch_own(const PagedAttnArgs& a, int own, hipStream_t st) {
-  if constexpr (std::is_same<DT, BF16>::value && SH != 3)
-    if (own == 0 || own == 3) return own == 0 ? launch_attention<DT, HD, SH, 0>(a, st) : launch_attention<DT, HD, SH, 3>(a, st);
-  return own == 1 ? launch_attention<DT, HD, SH, 1>(a, st) : launch_attention<DT, HD, SH, 2>(a, st);
+  if constexpr (std::is_same<DT, BF16>::value) {
+    if constexpr (SH != 3)
+      if (own != 1) return own == 0 ? launch_attention<DT, HD, SH, 0>(a, st) : launch_attention<DT, HD, SH, 3>(a, st);
+  } else {
+    if (own == 2) return launch_attention<DT, HD, SH, 2>(a, st);
+    if constexpr (SH == 0)
+      if (own > 3) return own == 4 ? launch_attention<DT, HD, SH, 4>(a, st) : launch_attention<DT, HD, SH, 5>(a, st);
+  }
+  return launch_attention<DT, HD, SH, 1>(a, st);
 }
 template <typename DT, int HD>
 static int launch_paged_attention(const PagedAttnArgs& a, const AttnCut& c, hipStream_t st) {

@@ -367,6 +367,15 @@ def test_attention_of_larger_batches(dtype, seqs, sb, heads):
     assert b.status == 0
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("heads", [(4, 4, 32), (6, 3, 64), (4, 2, 128)])
+@pytest.mark.parametrize("rows", [9, 23])
+def test_attention_of_many_short_sequences(dtype, heads, rows):
+    b = Batch([(n * 7 % 110, 1 + n % rows) for n in range(150)], *heads, 16, dtype, seed=rows, pad=2)
+    b.check(b.run())
+    assert b.status == 0
+
+
 @pytest.mark.parametrize("bt", [16, 32, 64, 256, 1024])
 def test_attention_block_sizes(bt):
     b = Batch([(bt - 1, 3), (bt, 1), (3 * bt + 5, 2)], 6, 2, 64, bt, BF16, seed=bt, shared_blocks=1)
