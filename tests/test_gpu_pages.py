@@ -376,6 +376,20 @@ def test_attention_of_many_short_sequences(dtype, heads, rows):
     assert b.status == 0
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_attention_of_thousands_of_sequences(dtype):
+    """More than the 4096 that two steps of a search tell apart, most without rows."""
+    rng = random.Random(1)
+    b = Batch([(rng.randrange(40), rng.choice([0, 0, 1, 3])) for _ in range(4200)], 2, 1, 32, 16, dtype, seed=2, shared_blocks=1)
+    out = b.run()
+    assert b.status == 0
+    with_rows = [s for s, r in enumerate(b.rows) if r]
+    for s in with_rows[:20] + with_rows[-20:] + rng.sample(with_rows, 60):
+        o, e = b.oracle(s, b.hd ** -0.5)
+        assert bool(((out[b.start[s]:b.start[s + 1]].double() - o).abs() <= e).all()), s
+    assert bool(torch.isfinite(out).all())
+
+
 @pytest.mark.parametrize("bt", [16, 32, 64, 256, 1024])
 def test_attention_block_sizes(bt):
     b = Batch([(bt - 1, 3), (bt, 1), (3 * bt + 5, 2)], 6, 2, 64, bt, BF16, seed=bt, shared_blocks=1)
@@ -671,3 +685,41 @@ def test_attention_over_a_cache_that_a_model_filled():
             k, v = kv.gather(s, layer, n)
             b.k.append(torch.from_numpy(k).cuda()), b.v.append(torch.from_numpy(v).cuda())
         b.check(ssd.ssd_paged_attention(kv.pages(layer), b.q, i32(b.lens), i32(b.start), table.cuda()))
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_calls_side_by_side_and_two_graphs(dtype):
+    """Two batches on two streams at once, then two captured calls replayed in turn with other work between, their lengths changed in place."""
+    import paper_2505_15380_amd as ssd
+    pair = [Batch([(900, 3), (20, 2), (333, 1)], 6, 2, 64, 16, dtype, seed=1, shared_blocks=8), Batch([(1500, 1), (64, 5)], 4, 2, 128, 32, dtype, seed=2)]
+    args = [(ssd.Pages(b.keys, b.values), b.q, i32(b.lens), i32(b.start), i32(b.table)) for b in pair]
+    kw = [dict(shared_table=i32(b.prefix) if b.sb else None, max_len=2000) for b in pair]
+    plain = [ssd.ssd_paged_attention(*a, **k) for a, k in zip(args, kw)]
+    for b, out in zip(pair, plain):
+        b.check(out)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(10):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(ssd.ssd_paged_attention(*args[i], **kw[i]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, plain[i]) for i in (0, 1) for o in outs[i])
+    graphs, held = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()], []
+    for i in (0, 1):
+        out = torch.empty_like(plain[i])
+        with torch.cuda.graph(graphs[i], stream=streams[i]):
+            ssd.ssd_paged_attention(*args[i], out=out, **kw[i])
+        held.append(out)
+    for turn in range(4):
+        lens = [torch.tensor(b.lens, dtype=torch.int32) - 7 * turn * torch.tensor([n > b.sb * b.bt + 60 for n in b.lens], dtype=torch.int32) for b in pair]
+        for i in (0, 1):
+            args[i][2].copy_(lens[i])
+            held[i].fill_(math.nan)
+        for i in (0, 1):
+            graphs[i].replay()
+        torch.ones(1 << 16, device="cuda").sum()
+        torch.cuda.synchronize()
+        for i in (0, 1):
+            assert torch.equal(held[i], ssd.ssd_paged_attention(*args[i], **kw[i])), (turn, i)
