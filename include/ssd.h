@@ -255,7 +255,7 @@ int ssd_block_tables(int n_seqs, int block_tokens, int n_blocks, int table_cap, 
 
 /* Rotary embedding and append (step a4 of a verification): for each of n_rows rows (0 allowed) the pairs (i, i + head_dim/2) of its n_q_heads query
  * heads and of its key heads are turned by the angles of dev_row_pos[r] - cosines and sines dev_rope [rope_positions][head_dim/2][2] fp32; null:
- * nothing is turned -, in fp32 and rounded once; queries go to dev_q_out (which may be dev_q), keys and values to slot dev_row_slot[r].  Rows are heads of
+ * nothing is turned -, in fp32 and rounded once; queries go to dev_q_out (which may be dev_q, with its stride), keys and values to slot dev_row_slot[r].  Rows are heads of
  * head_dim behind each other, `stride` elements from row to row (columns of one QKV product as well), beginning at multiples of 16 bytes.
  * n_q_heads 0: keys and values alone.  A row with a negative position is left out, one with a negative slot is not appended; a slot outside the pool
  * or a position outside dev_rope is left out and ORed to dev_status[0] (may be null).  Slots >= 0 are distinct: of two rows with one slot either

@@ -339,6 +339,11 @@ __global__ void __launch_bounds__(BLOCK) k_rope_append(RopeAppendArgs a, int v_w
     if (h >= heads || (!is_q && slot < 0)) break;
     T* dst = (is_q ? (T*)a.q_out + row * a.q_out_stride + h * hd
                    : (T*)a.p.keys + (((size_t)(slot >> a.p.bt_shift) * a.p.nkv + (h - a.nq)) * a.p.bt + (slot & (a.p.bt - 1))) * hd) + d;
+    if (!a.rope) {                                         // (as it is: times 1, less 0 times the other, is not the same for infinities)
+      *(u32x4*)dst = lo[k];
+      *(u32x4*)(dst + half) = hi[k];
+      continue;
+    }
     float x[N], y[N], u[N], w[N];
     Unit<DT>::get(lo[k], x);
     Unit<DT>::get(hi[k], y);

@@ -87,6 +87,7 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
   if (n_q_heads > 0) {
     if (int rc = check_rows("q", dev_q, q_stride, n_q_heads, a.p, pages->dtype)) return rc;
     if (int rc = check_rows("q_out", dev_q_out, q_out_stride, n_q_heads, a.p, pages->dtype)) return rc;
+    if (dev_q_out == dev_q && q_out_stride != q_stride && n_rows > 1) return fail(SSD_EINVAL, "q_out is q, but its rows are %zu apart, not %zu", q_out_stride, q_stride);
   }
   a.q = dev_q; a.k = dev_k; a.v = dev_v; a.q_out = dev_q_out;
   a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.q_out_stride = q_out_stride;

@@ -208,6 +208,23 @@ def test_rope_append(dtype, nq, nkv, hd, bt, n, packed, in_place):
     assert torch.equal(values, want_v)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_rope_append_without_angles_copies(dtype):
+    """Bit by bit, whatever the values are."""
+    import paper_2505_15380_amd as ssd
+    keys = torch.zeros((4, 2, 16, 64), dtype=dtype, device="cuda")
+    values = torch.zeros((4, 2, 64, 16), dtype=dtype, device="cuda")
+    x = torch.randn((20, 8, 64), device="cuda").to(dtype)
+    x[3, :, 40:] = math.inf
+    x[5, 1, 7], x[6, 6, 60], x[7, 3, :] = math.nan, -math.inf, -0.0
+    slot = torch.randperm(64)[:20]
+    q = ssd.ssd_rope_append(ssd.Pages(keys, values), i32(range(20)), i32(slot), x[:, 4:6], x[:, 6:], q=x[:, :4])
+    same = lambda a, b: torch.equal(a.contiguous().view(torch.int16 if dtype == BF16 else torch.int32), b.contiguous().view(torch.int16 if dtype == BF16 else torch.int32))      # noqa: E731
+    assert same(q, x[:, :4])
+    b, t = slot.cuda() // 16, slot.cuda() % 16
+    assert same(keys[b, :, t], x[:, 4:6]) and same(values[b, :, :, t], x[:, 6:])
+
+
 def test_rope_append_leaves_out_what_lies_outside():
     import paper_2505_15380_amd as ssd
     n, nkv, hd, bt = 6, 2, 64, 16

@@ -44,7 +44,7 @@ APPEND = dict(pages=None, n_rows=3, nq=4, q=P, qs=256, k=P, ks=128, v=P, vs=128,
 @pytest.mark.parametrize("change, code", [
     (dict(n_rows=-1), EINVAL), (dict(n_rows=(1 << 24) + 1), EINVAL), (dict(nq=-1), EINVAL), (dict(q=None), EINVAL), (dict(q_out=None), EINVAL), (dict(k=None), EINVAL),
     (dict(v=None), EINVAL), (dict(pos=None), EINVAL), (dict(slot=None), EINVAL), (dict(positions=0), EINVAL), (dict(qs=255), EINVAL), (dict(qs=260), EINVAL), (dict(os=128), EINVAL),
-    (dict(ks=120), EINVAL), (dict(vs=132), EINVAL), (dict(k=P + 8), EINVAL), (dict(q=P + 2), EINVAL),
+    (dict(ks=120), EINVAL), (dict(vs=132), EINVAL), (dict(k=P + 8), EINVAL), (dict(q=P + 2), EINVAL), (dict(os=264), EINVAL),
 ])
 def test_rope_append_refuses(lib, change, code):
     pg = pages()
