@@ -673,6 +673,17 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
       }
       return __any(large) != 0;
     };
+    // The values' operands are asked for ahead of the weights, which take longer than LDS does, where there are registers for them (with QS 2 it gains
+    // nothing): seven prompts 66.8 -> 63.8 us in a graph, 9 sequences of up to 919 rows with heads of 128 38.5 -> 35.5, 2 % in the mean over 29 calls.
+    auto values_of = [&](int k, int d) { return __builtin_bit_cast(bf16x8, kv_lds[it & 1][1][2 * t0 + k][d][2 * c + (h ^ (c >> 3 & 1))]); };
+    bf16x8 vf[QS == 1 ? 2 * NT : 1][J];
+    if constexpr (QS == 1) {
+#pragma unroll
+      for (int k = 0; k < 2 * NT; ++k)
+#pragma unroll
+        for (int d = 0; d < J; ++d) vf[k][d] = values_of(k, d);
+      __builtin_amdgcn_sched_barrier(0);                   // (or they are made where they are used)
+    }
     if (first || weigh(std::false_type())) weigh(std::true_type());
     first = false;
 #pragma unroll
@@ -681,9 +692,9 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
     for (int k = 0; k < 2 * NT; ++k)
 #pragma unroll
       for (int d = 0; d < J; ++d) {
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, kv_lds[it & 1][1][2 * t0 + k][d][2 * c + (h ^ (c >> 3 & 1))]);
+        const bf16x8 v = QS == 1 ? vf[QS == 1 ? k : 0][d] : values_of(k, d);
 #pragma unroll
-        for (int x = 0; x < QS; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p[x][k], o[x][d], 0, 0, 0);
+        for (int x = 0; x < QS; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[x][k], o[x][d], 0, 0, 0);
       }
   }
   if (__any(bad) && lane == 0 && a.status) atomicOr(a.status, ST_PAGE);
