@@ -19,10 +19,9 @@
 // What bounds a call (0.5B heads, 14 x 64 over 2, bf16, one MI355X; kernel times):
 //   few rows      the dependent steps - lengths, table, keys, scores, values, LDS - of which one token over 1024 positions takes 8.3 us; 16 x 7 rows over 256 to 4096 positions 11.5
 //                 us and 4.0 for the merge, where the bytes would take 3.1
-//   a prefix      of 16384 positions for 256 x 5 rows: 97 us, 780 TFLOP/s; the matrix units are busy for 35 % of that, the vector units (weights: a power of two, a product, half a
+//   a prefix      of 16384 positions for 256 x 5 rows: 96 us, 790 TFLOP/s; the matrix units are busy for 35 % of that, the vector units (weights: a power of two, a product, half a
 //                 conversion and half a sum each) for 45 %, and two waves of a SIMD hardly overlap the one with the other
-//   prompts       seven of 100 to 2001 rows behind 1024 positions: 70 us, 630 TFLOP/s, 26 and 36 %: the same, and compute units with four workgroups
-//                 beside ones with three
+//   prompts       seven of 100 to 2001 rows behind 1024 positions: 68 us, 650 TFLOP/s, 28 and 38 %: the same, and compute units with more workgroups than others
 #pragma once
 #include <type_traits>
 
