@@ -186,7 +186,7 @@ __device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, 
     if (blk >= 0) {
       const T* kp = (const T*)a.p.keys + (((size_t)blk * a.p.nkv + kvh) * a.p.bt + (key & tmask)) * HD;
       float dot = 0.f;
-#pragma unroll 1
+#pragma unroll 8
       for (int d = 0; d < HD; ++d) dot = fmaf(DT::ld(q + d), DT::ld(kp + d), dot);
       s = a.scale2 == 0.f ? 0.f : dot * a.scale2;
     }
@@ -200,14 +200,25 @@ __device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, 
     }
     const float weight = __builtin_amdgcn_exp2f(s - mx);
     sum += wave_sum(weight);
+    const int n = min(64, end - k0);
 #pragma unroll 1
-    for (int i = 0; i < min(64, end - k0); ++i) {
-      const int b = __builtin_amdgcn_readlane(blk, i);
-      if (b < 0) continue;
-      const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), i));
-      const T* vp = (const T*)a.p.values + (((size_t)b * a.p.nkv + kvh) * HD + dim) * a.p.bt + ((k0 + i) & tmask);
+    for (int i = 0; i < n; i += 8) {                       // (eight keys' values asked for at once)
+      float v[8][D];
 #pragma unroll
-      for (int j = 0; j < D; ++j) acc[j] = fmaf(f, DT::ld(vp + 64 * j * a.p.bt), acc[j]);
+      for (int e = 0; e < 8; ++e) {
+        const int key_i = min(i + e, n - 1), b = max(__builtin_amdgcn_readlane(blk, key_i), 0);
+        const T* vp = (const T*)a.p.values + (((size_t)b * a.p.nkv + kvh) * HD + dim) * a.p.bt + ((k0 + key_i) & tmask);
+#pragma unroll
+        for (int j = 0; j < D; ++j) v[e][j] = DT::ld(vp + 64 * j * a.p.bt);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int key_i = min(i + e, n - 1);
+        if (i + e >= n || __builtin_amdgcn_readlane(blk, key_i) < 0) continue;
+        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), key_i));
+#pragma unroll
+        for (int j = 0; j < D; ++j) acc[j] = fmaf(f, v[e][j], acc[j]);
+      }
     }
   }
   const size_t at = ((size_t)row * a.nq + head) * a.P + w.slot;
