@@ -361,6 +361,10 @@ int ssd_prompt_gemm_plan(int kind, int rows, int n, int k, int cus, int plan[4],
  * units?  1 or 0. */
 int ssd_resident_fits(const int* running, int n, int stream, int wgs, int cus);
 int ssd_attention_plan(int head_dim, int n_q_heads, int n_kv_heads, int n_seqs, int rows, int prompt_positions, int cus, int plan[3]);
+/* What ssd_paged_attention runs for such a call: plan = {how the shared prefix is read: 0 in line with each sequence's own positions, 1 and 2 tiles of 128 and 256 packed rows (row x
+ * query head of a group), 3 streams; how a sequence's own are: 0 and 3 tiles of 128 and 64 packed rows, 1 and 2 streams of up to 16 and 32, 4 and 5 the same of four
+ * waves; parts of the prefix; parts of a row at most, those among them: 1 needs no workspace}. */
+int ssd_paged_attention_plan(const ssd_pages* pages, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks, int plan[4]);
 
 const char* ssd_strerror(int code);
 const char* ssd_last_error(void);

@@ -14,6 +14,7 @@ EXPORTED_SYMBOLS = [
     "ssd_verify_noalloc", "ssd_kv_clear_error", "ssd_kv_test_hook", "ssd_cycle_create", "ssd_cycle_launch", "ssd_cycle_captures", "ssd_cycle_destroy",
     "ssd_gemm_plan", "ssd_gemm_blocks", "ssd_prompt_gemm_plan", "ssd_attention_plan", "ssd_resident_fits",
     "ssd_block_tables", "ssd_rope_append", "ssd_paged_attention_workspace_bytes", "ssd_paged_attention",
+    "ssd_paged_attention_plan",
 ]
 
 
@@ -101,6 +102,7 @@ def load_library():
         "ssd_paged_attention_workspace_bytes": (sz, [C.POINTER(_Pages), i32, i32, i32, i32, i32]),
         "ssd_paged_attention": (i32, [C.POINTER(_Pages), i32, C.c_float, i32, i32, i32, i32p, i32p, i32p, i32, i32, i32p, i32p, vp, sz, vp, sz,
                                       vp, sz, i32p, vp]),
+        "ssd_paged_attention_plan": (i32, [C.POINTER(_Pages), i32, i32, i32, i32, i32, C.POINTER(C.c_int)]),
         "ssd_strerror": (C.c_char_p, [i32]),
         "ssd_last_error": (C.c_char_p, []),
     }
@@ -502,6 +504,13 @@ def paged_attention_workspace(pages, n_q_heads, n_seqs, n_rows, max_len, shared_
     if need == C.c_size_t(-1).value:
         raise SSDError(-1, load_library().ssd_last_error().decode())
     return need
+
+
+def paged_attention_plan(pages, n_q_heads, n_seqs, n_rows, max_len, shared_blocks=0):
+    """What ssd_paged_attention runs for such a call: (kind of the shared prefix's workgroups, kind of the sequences' own, parts of the prefix, parts of a row)."""
+    plan = (C.c_int * 4)()
+    _check(load_library().ssd_paged_attention_plan(pages.ref, n_q_heads, n_seqs, n_rows, max_len, shared_blocks, plan))
+    return tuple(plan)
 
 
 PROFILE_KINDS = {"qkv": 0, "attention": 1, "o": 2, "gate_up": 3, "down": 4, "head": 5, "persistent": 6}

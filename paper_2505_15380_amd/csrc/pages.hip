@@ -222,6 +222,15 @@ extern "C" size_t ssd_paged_attention_workspace_bytes(const ssd_pages* pages, in
   return attention_ws(cut_attention(pages->dtype, p.hd, p.nkv, n_q_heads / p.nkv, n_seqs, n_rows, max_len, shared_blocks * p.bt), n_rows, n_q_heads, p.hd);
 }
 
+extern "C" int ssd_paged_attention_plan(const ssd_pages* pages, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks, int plan[4]) {
+  Pages p;
+  if (int rc = check_attention(pages, p, n_q_heads, n_seqs, n_rows, max_len, shared_blocks)) return rc;
+  if (!plan || n_rows < 1) return fail(SSD_EINVAL, plan ? "a call without rows has no plan" : "null argument");
+  const AttnCut c = cut_attention(pages->dtype, p.hd, p.nkv, n_q_heads / p.nkv, n_seqs, n_rows, max_len, shared_blocks * p.bt);
+  plan[0] = c.sh; plan[1] = c.own; plan[2] = c.P_sh; plan[3] = c.P;
+  return SSD_OK;
+}
+
 template <typename DT, int HD, int SH, int OWN>
 static int launch_attention(const PagedAttnArgs& a, hipStream_t st) {
   const long long wgs = ((long long)a.sh_slots * a.P_sh + (long long)a.own_slots * (a.P - a.P_sh)) * a.p.nkv;

@@ -1,0 +1,184 @@
+"""Every kernel of ssd_paged_attention against attention in 64 bits: the batches of page_plans, ragged, some sequences outside the prefix."""
+import math
+import random
+
+import pytest
+import torch
+
+from tests.page_plans import BATCHES, BF16, FP32, KERNELS, name, ragged
+from tests.test_gpu_pages import U16, U32, Batch
+
+pytestmark = pytest.mark.gpu
+
+SMALLEST = [(k, bs[0]) for k, bs in KERNELS.items()]       # of every kernel
+
+
+@pytest.fixture(scope="module", autouse=True)
+def need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2505_15380_amd as pkg
+    pkg.load_library()
+
+
+class Planned(Batch):
+    """A batch of page_plans; every fifth sequence, where there are enough, does not have the prefix in front."""
+
+    def __init__(self, case):
+        (dtype, hd, *self.kernel), (nq, nkv, B, per, own, sb, bt, *self.parts) = case
+        seqs, self.max_len = ragged(case[1])
+        super().__init__(seqs, nq, nkv, hd, bt, dtype, seed=B + own, shared_blocks=sb, joins=[s % 5 != 4 for s in range(B)] if sb else None, pad=2)
+
+    def run(self, **kw):
+        import paper_2505_15380_amd as ssd
+        plan = ssd.paged_attention_plan(ssd.Pages(self.keys, self.values), self.nq, len(self.rows), len(self.q) - 2, self.max_len, self.sb)
+        assert plan == (*self.kernel, *self.parts)
+        out = torch.full_like(self.q, 7.0)
+        # (the rows behind the last one are no rows of the call)
+        super().run(q=self.q[:-2], out=out[:-2], max_len=self.max_len, **kw)
+        assert bool((out[-2:] == 7.0).all())
+        return out[:-2]
+
+    def mark(self):
+        """1000 in one dim of the values at the edges of 64 keys, of the prefix and at the new rows: a key that is dropped, taken twice or seen too early moves that dim by far
+        more than the roundings."""
+        at = self.sb * self.bt
+        for s, (n, r) in enumerate(zip(self.lens, self.rows)):
+            p = torch.arange(n + r)
+            p = p[(p % 64 == 0) | (p % 64 == 63) | (p >= n) | (p == at - 1) | (p == at)]
+            d = (5 * p + p // 64) % self.hd
+            blocks = self.table[s].clone()
+            if self.sb and self.joins[s]:
+                blocks[:self.sb] = torch.tensor(self.prefix)
+            p, d, b = p.cuda(), d.cuda(), blocks[p // self.bt].cuda()
+            self.values[b, :, d, p % self.bt] = 1000.0
+            self.v[s][p, :, d] = 1000.0
+
+    def oracle(self, s, scale, keep=None):
+        o, e = super().oracle(s, scale, keep)
+        # Tiles divide by the sum of the rounded weights p (1 + d), |d| <= u: off by sum p d (v - o) <= u (sum p |v| + |o|), the second term of which is added here.
+        return o, e + (U16 * (1 + U16) * o.abs() if self.dtype == BF16 else 0)
+
+    def block(self, s, i):
+        return self.prefix[i] if self.sb and self.joins[s] and i < self.sb else int(self.table[s, i])
+
+
+@pytest.mark.parametrize("case", BATCHES, ids=name)
+def test_kernel(case):
+    b = Planned(case)
+    b.mark()
+    out = b.run()
+    assert b.status == 0
+    b.check(out)
+    assert torch.equal(out, b.run())
+
+
+@pytest.mark.parametrize("case", SMALLEST, ids=name)
+def test_kernel_without_some_pages(case):
+    """A block of the prefix, one of a sequence's own, and all that a row sees."""
+    b = Planned(case)
+    n_blocks, bt = b.keys.shape[0], b.bt
+    keep = [torch.ones(n + r, dtype=torch.bool, device="cuda") for n, r in zip(b.lens, b.rows)]
+    bad = random.Random(1)
+    if b.sb:
+        gone = b.sb // 2
+        b.prefix[gone] = n_blocks + 7
+        for s, j in enumerate(b.joins):
+            if j:
+                keep[s][gone * bt:(gone + 1) * bt] = False
+    for s, (n, r) in enumerate(zip(b.lens, b.rows)):
+        first = b.sb if b.sb and b.joins[s] else 0
+        have = -(-(n + r) // bt)
+        if s % 3 == 0 and have > first:
+            i = bad.randrange(first, have)
+            b.table[s, i] = bad.choice([-1, -2 ** 31, n_blocks, 2 ** 31 - 1])
+            keep[s][i * bt:(i + 1) * bt] = False
+    alone = next((s for s, r in enumerate(b.rows) if r and not (b.sb and b.joins[s])), None)
+    if alone is not None:
+        b.table[alone] = -1
+        keep[alone][:] = False
+    out = b.run()
+    b.check(out, keep=keep)
+    assert b.status == 16
+    if alone is not None:
+        assert bool((out[b.start[alone]:b.start[alone + 1]] == 0).all())
+
+
+@pytest.mark.parametrize("case", SMALLEST, ids=name)
+def test_kernel_and_what_is_not_finite(case):
+    """Infinities and NaN at new rows' positions are nothing to the rows before them, and come out at those that see them."""
+    b = Planned(case)
+    G, last = b.nq // b.nkv, b.nkv - 1
+    expect = torch.zeros((b.n, b.nq, b.hd), dtype=torch.float64, device="cuda")
+    seqs = [s for s, r in enumerate(b.rows) if r >= 2]
+    assert seqs
+    for s in seqs:
+        n, r = b.lens[s], b.rows[s]
+        put = [(r // 2, 3, math.inf), (r // 2, 5, math.nan), (r // 2, 8, -math.inf), (r // 2, 9, math.inf), (r - 1, 9, -math.inf), (r - 1, 31, math.inf)]
+        if s % 4 == 3:                                     # a key instead
+            b.keys[b.block(s, (n + r - 1) // b.bt), last, (n + r - 1) % b.bt] = math.nan
+            expect[b.start[s] + r - 1, b.nq - G:] = math.nan
+            continue
+        if r == 2:                                         # (of two rows, the same one)
+            put = [x for x in put if x[1] != 9]
+        for row, d, x in put:
+            b.values[b.block(s, (n + row) // b.bt), last, d, (n + row) % b.bt] = x
+            expect[b.start[s] + row:b.start[s + 1], b.nq - G:, d] += x
+    out = b.run().double()
+    assert b.status == 0
+    code = lambda t: torch.where(torch.isfinite(t), 0, t).nan_to_num(nan=1.0, posinf=2.0, neginf=3.0)      # noqa: E731
+    assert torch.equal(code(out), code(expect))
+    for s, r in enumerate(b.rows):
+        if not r:
+            continue
+        o, e = b.oracle(s, b.hd ** -0.5)
+        at = slice(b.start[s], b.start[s + 1])
+        assert bool((((out[at] - o).abs() <= e) | (expect[at] != 0)).all()), s
+
+
+@pytest.mark.parametrize("heads, seqs, sb", [((14, 2, 64), [(3000, 7), (2500, 30), (500, 90)], 0), ((12, 2, 128), [(n * 37 % 900, 8) for n in range(40)], 100),
+                                             ((4, 4, 32), [(2000, 1)] * 60, 200), ((14, 2, 64), [(n % 300, 5) for n in range(250)], 300)])
+def test_error_of_a_whole_result(heads, seqs, sb):
+    """The norm of the error: an output is rounded once, and so is each weight.  A rounding of x by at most u |x| is a uniform one of at most half a step, which is u |x| / sqrt(3) in the root of
+    the mean square or less (less by up to two, as x lies between powers of two); of one row's weights p they add up as sqrt(sum (p |v - o|)^2), or with |v| where the sum is that of the weights before they
+    are rounded, since they are independent.  10 % for the spread of the
+    mean over a few thousand rows, and for what is in fp32."""
+    b = Batch(seqs, *heads, 16, BF16, seed=sb + len(seqs), shared_blocks=sb)
+    out = b.run().double()
+    err = size = 0.0
+    G = b.nq // b.nkv
+    for s, r in enumerate(b.rows):
+        o, _ = b.oracle(s, b.hd ** -0.5)
+        k, v = (t.double().repeat_interleave(G, 1).transpose(0, 1).contiguous() for t in (b.k[s], b.v[s]))
+        q = b.q[b.start[s]:b.start[s + 1]].double().transpose(0, 1).contiguous()
+        w = torch.bmm(q, k.transpose(1, 2).contiguous()) * b.hd ** -0.5
+        p = torch.softmax(w.masked_fill(torch.arange(k.shape[1], device="cuda") > b.lens[s] + torch.arange(r, device="cuda")[:, None], -math.inf), -1)
+        oo = o.transpose(0, 1).contiguous()
+        # |v - o|^2 = |v|^2 - 2 v.o + |o|^2
+        v2 = (v * v).sum(-1)[:, None]
+        far = v2 - 2 * torch.bmm(oo, v.transpose(1, 2).contiguous()) + (oo * oo).sum(-1)[..., None]
+        size += float((o * o).sum() + (p * p * torch.maximum(far, v2)).sum())
+        err += float(((out[b.start[s]:b.start[s + 1]] - o) ** 2).sum())
+    assert math.sqrt(err) <= 1.1 * U16 / math.sqrt(3) * math.sqrt(size)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_large_scores_pick_their_key(dtype):
+    """Scores of 1e5: where the largest is apart from the next one by 200, far more than the roundings of a score (hd + 3 of 2^-24 of 1e6), its value is the result: times its
+    weight, rounded (bf16: to bf16), and by its weight, the sum (a division and a product), and rounded to the type of the output."""
+    b = Batch([(70, 3), (700, 20), (3, 90)], 4, 2, 64, 16, dtype, seed=9, spread=3e4)
+    out = b.run()
+    apart = 0
+    for s in range(3):
+        k, v = (t.double().repeat_interleave(2, 1).transpose(0, 1).contiguous() for t in (b.k[s], b.v[s]))
+        q = b.q[b.start[s]:b.start[s + 1]].double().transpose(0, 1).contiguous()
+        w = torch.bmm(q, k.transpose(1, 2).contiguous()) * 0.125
+        w = w.masked_fill(torch.arange(k.shape[1], device="cuda") > b.lens[s] + torch.arange(q.shape[1], device="cuda")[:, None], -math.inf)
+        top, at = w.topk(2, -1)
+        clear = top[..., 0] - top[..., 1] > 200
+        want = torch.gather(v, 1, at[..., :1].expand(-1, -1, 64)).transpose(0, 1)
+        got = out[b.start[s]:b.start[s + 1]].double()
+        clear = clear.transpose(0, 1)
+        assert bool(((got - want).abs() <= want.abs() * (2.1 * U16 if dtype == BF16 else 4 * U32))[clear].all())
+        apart += int(clear.sum())
+    assert apart > 300
