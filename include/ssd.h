@@ -273,8 +273,9 @@ int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads, const voi
  * bits.  Sums and softmax are fp32; with bf16 pages the weights are rounded to bf16 for their product with the values.
  *   A position whose block is not in the pool or not in the table is left out, and SSD_STATUS_PAGE ORed to dev_status[0] (may be null); a row that has
  * no position left gets zeros.  What lies in positions that a row does not see, infinities and NaN too, does not reach it.
- *   dev_ws: ssd_paged_attention_workspace_bytes(), which may be 0 (dev_ws may be null then), and (size_t)-1 for arguments that the call refuses; calls
- * that may overlap need workspaces of their own.  n_rows * n_q_heads <= 2^26, n_seqs <= 65536, table_cap * block_tokens <= 2^30. */
+ *   dev_ws: ssd_paged_attention_workspace_bytes() is enough for every call over such pages and heads with no more sequences, rows, max_len and shared blocks (one workspace, sized for
+ * the largest step, does for all of them); it may be 0 (dev_ws may be null then), and is (size_t)-1 for arguments that the call refuses.  A call itself asks for
+ * n_rows * n_q_heads * parts * (head_dim + 2) floats if it is cut into parts (ssd_paged_attention_plan).  Calls that may overlap need workspaces of their own.  n_rows * n_q_heads <= 2^26, n_seqs <= 65536, table_cap * block_tokens <= 2^30. */
 size_t ssd_paged_attention_workspace_bytes(const ssd_pages* pages, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks);
 int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float scale, int n_seqs, int n_rows, int max_len, const int32_t* dev_len,
                         const int32_t* dev_row_start, const int32_t* dev_table, int table_cap, int shared_blocks, const int32_t* dev_shared_table,

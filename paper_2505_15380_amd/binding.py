@@ -476,7 +476,7 @@ def ssd_rope_append(pages, row_pos, row_slot, k, v, q=None, rope=None, q_out=Non
 def ssd_paged_attention(pages, q, lens, row_start, table, scale=None, shared_table=None, shared=None, max_len=None, out=None, ws=None, status=None):
     """Attention of q [n_rows, n_q_heads, head_dim] over the pages of its sequences: lens [n_seqs], row_start [n_seqs + 1], table [n_seqs, cap], and
     shared_table [shared_blocks], shared [n_seqs] of a common prefix, int32.  scale: 1 / sqrt(head_dim) unless given.  max_len: about the largest len + rows (what the table
-    holds unless given).  ws: a uint8 device tensor of paged_attention_workspace() bytes, unless it is to be allocated here.  Returns out."""
+    holds unless given).  ws: a uint8 device tensor of paged_attention_workspace() bytes, unless what this call needs is to be allocated here.  Returns out."""
     n, nq, hd = q.shape
     B, cap = table.shape
     dev, a = _device_is_current(pages.keys), _int_array
@@ -487,8 +487,8 @@ def ssd_paged_attention(pages, q, lens, row_start, table, scale=None, shared_tab
     if max_len is None:
         max_len = cap * pages.block_tokens
     if ws is None:
-        need = paged_attention_workspace(pages, nq, B, n, max_len, sb)
-        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        parts = paged_attention_plan(pages, nq, B, n, max_len, sb)[3] if n else 1
+        ws = torch.empty(n * nq * parts * (hd + 2) * 4, dtype=torch.uint8, device=q.device) if parts > 1 else None
     elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
         raise SSDError(-1, "ws is a uint8 tensor in one piece on the device of the pages")
     _check(load_library().ssd_paged_attention(
@@ -499,7 +499,7 @@ def ssd_paged_attention(pages, q, lens, row_start, table, scale=None, shared_tab
 
 
 def paged_attention_workspace(pages, n_q_heads, n_seqs, n_rows, max_len, shared_blocks=0):
-    """Bytes of ssd_paged_attention's workspace for such a call."""
+    """Bytes of a workspace that is enough for ssd_paged_attention of as many sequences, rows, positions and shared blocks, or fewer."""
     need = load_library().ssd_paged_attention_workspace_bytes(pages.ref, n_q_heads, n_seqs, n_rows, max_len, shared_blocks)
     if need == C.c_size_t(-1).value:
         raise SSDError(-1, load_library().ssd_last_error().decode())

@@ -110,14 +110,23 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
 // `longest`: of the workgroups, alone on a compute unit; `load`: of all of them, spread over 256 compute units.  The terms were fitted to 7100 cuts of 126 calls (1 to 256 sequences,
 // 1 to 7600 rows, 9 to 16888 positions), but for the 3.8, of which a graph takes 2.3 and a launch by itself more.  The cut that is picked takes 5 % more time
 // in the mean than the best that was measured, and at most 25 %; rules on the rows of a sequence took 24 %, and up to three times.
+//   What the parts leave for the merge takes no more than a workspace that grows with rows, length and prefix, so that one for a caller's largest call does for every smaller one:
+// rows x heads x parts stay below twice the rows x heads (a shared prefix and own keys) + 2^18, which is 1024 workgroups of 256 rows.  Of 300000 sizes, up to 65536 rows and 512 heads, it
+// changes the cut of 1.4 %; by the estimate the mean call then takes 0.03 % longer, and the worst 11 %.
+constexpr int PA_PARTS = 32;                               // of a source at most: no more than 64 of a row
+static long long partial_rows(long long row_heads, int max_len, int shared_positions) {
+  const int parts = std::min(PA_PARTS, cdiv(max_len, PA_CHUNK)) + std::min(PA_PARTS, cdiv(shared_positions, PA_CHUNK));
+  return parts < 2 ? 0 : std::min(row_heads * parts, 2 * row_heads + (1 << 18));
+}
 struct AttnCut {
   int sh, own;                                             // k_paged_attention's SH and OWN
   bool in_line;
   int P, P_sh, sh_chunks, own_chunks, sh_slots, own_slots;
 };
 static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, int n_rows, int max_len, int shared_positions) {
-  constexpr int PARTS[] = {1, 2, 3, 4, 5, 6, 7, 8, 12, 16, 32};            // of a source: no more than 64 of a row
+  constexpr int PARTS[] = {1, 2, 3, 4, 5, 6, 7, 8, 12, 16, PA_PARTS};
   const bool b16 = dtype == SSD_DTYPE_BF16;
+  const int most = n_rows ? (int)std::min(2ll + (1 << 18) / ((long long)n_rows * nkv * group), 2ll * PA_PARTS) : 1;        // parts of a row
   const int packed = n_rows * group, each = cdiv(packed, n_seqs), sh_n = cdiv(shared_positions, PA_CHUNK);
   const float part_us = 0.195f * (float)n_rows * nkv * group * (hd + 2) * 8e-6f;
   // A chunk of a workgroup of 128 rows by tiles (bf16), alone and as a share of a full compute unit; a step of a
@@ -178,6 +187,7 @@ static AttnCut cut_attention(int dtype, int hd, int nkv, int group, int n_seqs, 
         Source& x = shared[sh ? sh - 1 : 0];
         auto us = [&](int i, int j) {
           const int parts = o.parts[i] + (sh ? x.parts[j] : 0);
+          if (parts > most) return 1e30f;
           const float longest = sh ? std::max(o.longest[i], x.longest[j]) : o.longest[i], load = o.load[i] + (sh ? x.load[j] : 0.f);
           return sqrtf(longest * longest + load * load) + (parts > 1 ? 3.8f + parts * part_us : 0.f);
         };
@@ -219,7 +229,7 @@ static size_t attention_ws(const AttnCut& c, int n_rows, int nq, int hd) { retur
 extern "C" size_t ssd_paged_attention_workspace_bytes(const ssd_pages* pages, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks) {
   Pages p;
   if (check_attention(pages, p, n_q_heads, n_seqs, n_rows, max_len, shared_blocks)) return (size_t)-1;
-  return attention_ws(cut_attention(pages->dtype, p.hd, p.nkv, n_q_heads / p.nkv, n_seqs, n_rows, max_len, shared_blocks * p.bt), n_rows, n_q_heads, p.hd);
+  return (size_t)partial_rows((long long)n_rows * n_q_heads, max_len, shared_blocks * p.bt) * (p.hd + 2) * sizeof(float);
 }
 
 extern "C" int ssd_paged_attention_plan(const ssd_pages* pages, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks, int plan[4]) {

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests.page_plans import BATCHES, BF16, FP32, KERNELS, name, ragged
-from tests.test_gpu_pages import U16, U32, Batch
+from tests.test_gpu_pages import U16, U32, Batch, serve
 
 pytestmark = pytest.mark.gpu
 
@@ -182,3 +182,35 @@ def test_large_scores_pick_their_key(dtype):
         assert bool(((got - want).abs() <= want.abs() * (2.1 * U16 if dtype == BF16 else 4 * U32))[clear].all())
         apart += int(clear.sum())
     assert apart > 300
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_one_workspace_for_steps_of_all_sizes(dtype):
+    """Sized for the largest, which itself needs none."""
+    import paper_2505_15380_amd as ssd
+    largest = Batch([(500, 64)] * 64, 14, 2, 64, 16, dtype, seed=5)
+    pages = ssd.Pages(largest.keys, largest.values)
+    most = ssd.paged_attention_workspace(pages, 14, 64, largest.n, 4096, 20)
+    ws = torch.full((most,), 255, dtype=torch.uint8, device="cuda")
+    assert ssd.paged_attention_plan(pages, 14, 64, largest.n, 564)[3] == 1
+    largest.check(largest.run(ws=ws))
+    cut = 0
+    for seqs, sb in (([(n * 50, 1) for n in range(64)], 0), ([(n * 9, 3) for n in range(40)], 20), ([(3000, 2)], 0), ([(100, 200), (7, 1)], 3)):
+        b = Batch(seqs, 14, 2, 64, 16, dtype, seed=sb, shared_blocks=sb)
+        cut += ssd.paged_attention_plan(pages, 14, len(seqs), b.n, max(n + r for n, r in zip(b.lens, b.rows)), sb)[3] > 1
+        out = b.run(ws=ws)
+        b.check(out)
+        assert torch.equal(out, b.run())
+    assert cut >= 2
+
+
+@pytest.mark.parametrize("dtype, heads, bt, voice, n_seqs", [(BF16, (14, 2, 64), 16, 4096, 30), (BF16, (4, 4, 32), 16, 1024, 40), (BF16, (4, 2, 128), 32, 2048, 40), (FP32, (2, 2, 64), 16, 1024, 30)])
+@pytest.mark.parametrize("graph", [False, True])
+def test_steps_of_a_served_batch_with_a_prefix_of_its_own(dtype, heads, bt, voice, n_seqs, graph):
+    """Served steps whose prefix is read once for all rows, in parts that are merged."""
+    import paper_2505_15380_amd as ssd
+    nq, nkv, hd = heads
+    pages = ssd.Pages(torch.empty((1, nkv, bt, hd), dtype=dtype, device="cuda"), torch.empty((1, nkv, hd, bt), dtype=dtype, device="cuda"))
+    sh, _, parts_sh, parts = ssd.paged_attention_plan(pages, nq, n_seqs, n_seqs * 20 + 5, voice + 6 * bt, voice // bt)
+    assert sh > 0 and parts_sh > 1 and parts > 1
+    serve(dtype, heads, bt, voice, n_seqs=n_seqs, steps=5, graph=graph)

@@ -1,6 +1,7 @@
 """Which kernel ssd_paged_attention picks.  CPU only: nothing is launched."""
 import ctypes as C
 import os
+import random
 import re
 
 import pytest
@@ -50,3 +51,21 @@ def test_plan_refuses_what_the_call_refuses(lib):
                  (ref, 14, 2, 2, 100, -1, plan), (ref, 14, 2, 2, 100, 0, None)):
         assert lib.ssd_paged_attention_plan(*args) == -1
         assert lib.ssd_last_error()
+
+
+def test_a_workspace_is_enough_for_every_smaller_call(lib):
+    """A caller asks once, for the largest step."""
+    rng = random.Random(2)
+    size = lambda lo, hi: min(hi, int(lo * (hi / lo) ** rng.random() * rng.choice([1, 1, 1.3])))      # noqa: E731
+    plan = (C.c_int * 4)()
+    for _ in range(20000):
+        nkv, group, hd, dtype, bt = rng.choice([1, 2, 4, 8]), rng.choice([1, 3, 6, 7, 8]), rng.choice([32, 64, 128]), rng.choice([BF16, BF16, 0]), rng.choice([16, 64])
+        ref, nq = C.byref(pages(dtype, hd, nkv, bt)), nkv * group
+        n_seqs, n_rows, max_len, sb = size(1, 2000), size(1, 30000), size(1, 60000), rng.choice([0, size(1, 1000)])
+        most = lib.ssd_paged_attention_workspace_bytes(ref, nq, n_seqs, n_rows, max_len, sb)
+        for _ in range(3):
+            small = size(1, n_rows)
+            assert lib.ssd_paged_attention_plan(ref, nq, size(1, n_seqs), small, size(1, max_len), rng.choice([0, sb, rng.randint(0, sb)]), plan) == 0
+            assert plan[3] == 1 or small * nq * plan[3] * (hd + 2) * 4 <= most
+    assert lib.ssd_paged_attention_workspace_bytes(ref, nq, 9, 0, 5000, 7) == 0
+    assert lib.ssd_paged_attention_workspace_bytes(ref, nq, 9, 4000, 64, 0) == 0                       # one chunk of keys: nothing to cut
