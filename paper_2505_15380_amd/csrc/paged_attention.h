@@ -33,7 +33,7 @@ namespace ssd {
 constexpr int PA_WAVES = 4, PA_THREADS = PA_WAVES * WAVE;        // of a workgroup of tiles; streams that are by themselves have twice as many
 constexpr int PA_CHUNK = 64;           // keys in which parts are counted
 constexpr float PA_LAZY = 8.0f, PA_LARGE = 256.0f;
-constexpr float PA_NONE = -3.0e38f;    // the reference of a row that has seen nothing
+constexpr float PA_NONE = -3.402823466e38f;                      // the reference of a row that has seen nothing: no score that is a number is below it
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 struct PagedAttnArgs {
@@ -169,19 +169,25 @@ __device__ __forceinline__ u32x4 factor_into(const PagedAttnArgs& a, u32x4 q, ui
 
 // Rows that share a tile do not all see its last keys.  The weight of a hidden key is 0, and 0 times a value that is not finite is NaN, so a row with such a key and a result
 // that is not finite is done over, by one wave, from the keys that it sees: the products then need no look at the values, and this is as rare as infinities in a cache are.
+//   So is a row whose weights sum up to 0 although there are keys before it: its blocks are missing, or all of its scores are -inf, and a softmax of these is NaN. Of a part, the
+// reference -inf says so, and becomes NaN if no other part has anything.
 __device__ __forceinline__ bool has_hidden(const Work& w, int G, int pr) { return !w.shared && w.len + pr / G + 1 < w.k_end; }
+__device__ __forceinline__ bool has_keys(const Work& w, int G, int pr) { return w.shared || w.k_begin < w.len + pr / G + 1; }
 __device__ __forceinline__ bool all_finite(f32x4 v) { return v[0] * 0.f + v[1] * 0.f + v[2] * 0.f + v[3] * 0.f == 0.f; }
 template <typename DT, int HD>
 __device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, int kvh, int G, int pr) {
   typedef typename DT::T T;
   constexpr int D = HD < 64 ? 1 : HD / 64;
-  const int lane = threadIdx.x & 63, dim = lane & (HD - 1), row = w.seq_r0 + pr / G, head = kvh * G + pr % G, end = min(w.len + pr / G + 1, w.k_end), tmask = a.p.bt - 1;
+  const int lane = threadIdx.x & 63, dim = lane & (HD - 1), row = w.seq_r0 + pr / G, head = kvh * G + pr % G, end = w.shared ? w.k_end : min(w.len + pr / G + 1, w.k_end), tmask = a.p.bt - 1;
   const T* q = (const T*)a.q + (size_t)row * a.q_stride + head * HD;
   float acc[D] = {}, mx = PA_NONE, sum = 0.f;
+  bool seen = false;
   for (int k0 = w.k_begin; k0 < end; k0 += 64) {
     const int key = k0 + lane;
     int bad = 0;
     const int blk = key < end ? checked_block(a, w, block_of(a, w, key), key, bad) : -1;
+    if (!__any(blk >= 0)) continue;
+    seen = true;
     float s = -INFINITY;
     if (blk >= 0) {
       const T* kp = (const T*)a.p.keys + (((size_t)blk * a.p.nkv + kvh) * a.p.bt + (key & tmask)) * HD;
@@ -222,10 +228,11 @@ __device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, 
     }
   }
   const size_t at = ((size_t)row * a.nq + head) * a.P + w.slot;
+  if (seen && sum == 0.f) mx = -INFINITY;
 #pragma unroll
   for (int j = 0; j < D; ++j) {
     if (lane >= HD) continue;
-    if (w.slot < 0) DT::st((T*)a.out + (size_t)row * a.out_stride + head * HD + dim + 64 * j, sum == 0.f ? 0.f : acc[j] / sum);
+    if (w.slot < 0) DT::st((T*)a.out + (size_t)row * a.out_stride + head * HD + dim + 64 * j, sum == 0.f ? (seen ? NAN : 0.f) : acc[j] / sum);
     else a.o_part[at * HD + dim + 64 * j] = acc[j];
   }
   if (w.slot >= 0 && lane == 0) { a.ml_part[at * 2] = mx; a.ml_part[at * 2 + 1] = sum; }
@@ -417,7 +424,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
     if (more) load_values(base_next, k_next);
   }
   if (__any(bad) && lane == 0 && a.status) atomicOr(a.status, ST_PAGE);
-  uint32_t again = 0;                                      // rows of which this lane has written something that is not finite
+  uint32_t again = 0, empty = 0;                           // rows of which this lane has written something that is not finite; whose weights sum up to 0
   float (*po)[16][HD + 4] = (float (*)[16][HD + 4])lds;
   float (*pm)[16] = (float (*)[16])(lds + 4 * 16 * (HD + 4)), (*pl)[16] = pm + 4;
 #pragma unroll
@@ -461,6 +468,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
       }
       const int pr = w.row0 + 16 * x + r, row = w.seq_r0 + pr / G, head = kvh * G + pr % G;
       if (!SHARED && !all_finite(acc)) again |= 1u << (16 * x + r);
+      if (sum == 0.f) empty |= 1u << (16 * x + r);
       if (w.slot < 0) {
         T* dst = (T*)a.out + (size_t)row * a.out_stride + head * HD + d;
         acc *= sum == 0.f ? 0.f : 1.f / sum;
@@ -473,11 +481,13 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
       }
     }
   }
-  if (!SHARED && __any(again)) {
+  if (__any(again | empty)) {
     // (one wave has written the whole of a row; it writes it again behind that)
     __builtin_amdgcn_s_waitcnt(0x0070);
-    for (int r = 0; r < rows; ++r)
-      if (__any(again >> r & 1) && has_hidden(w, G, w.row0 + r)) redo_row<DT, HD>(a, w, kvh, G, w.row0 + r);
+    for (int r = 0; r < rows; ++r) {
+      const int pr = w.row0 + r;
+      if ((__any(again >> r & 1) && has_hidden(w, G, pr)) || (__any(empty >> r & 1) && has_keys(w, G, pr))) redo_row<DT, HD>(a, w, kvh, G, pr);
+    }
   }
 }
 
@@ -741,7 +751,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
         }
     }
   }
-  unsigned long long again[QS];                            // lanes that have written something that is not finite
+  unsigned long long again[QS], empty[QS];                 // lanes that have written something that is not finite; whose rows' weights sum up to 0
 #pragma unroll
   for (int x = 0; x < QS; ++x) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[x]), __float_as_uint(l[x]), false, false);
@@ -752,6 +762,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
 #pragma unroll
       for (int e = 0; e < 4; ++e) any += f32x4{o[x][d][4 * e], o[x][d][4 * e + 1], o[x][d][4 * e + 2], o[x][d][4 * e + 3]} * 0.f;
     again[x] = __ballot(!SHARED && !all_finite(any));
+    empty[x] = __ballot(ls == 0.f);
     if (w0 + 32 * x + c >= w.n_packed) continue;
     // dims 32 d + 8 e + 4 h .. + 3 in registers 4 e ..
     if (w.slot < 0) {
@@ -772,15 +783,13 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
       if (h == 0) { a.ml_part[at * 2] = m[x]; a.ml_part[at * 2 + 1] = ls; }
     }
   }
-  if constexpr (!SHARED) {
 #pragma unroll
-    for (int x = 0; x < QS; ++x) {
-      if (!again[x]) continue;
-      __builtin_amdgcn_s_waitcnt(0x0070);
-      for (int r = 0; r < 32; ++r) {
-        const int pr = w0 + 32 * x + r;
-        if (((again[x] | again[x] >> 32) >> r & 1) && pr < w.n_packed && has_hidden(w, G, pr)) redo_row<BF16, HD>(a, w, kvh, G, pr);
-      }
+  for (int x = 0; x < QS; ++x) {
+    if (!(again[x] | empty[x])) continue;
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    for (int r = 0; r < 32; ++r) {
+      const int pr = w0 + 32 * x + r;
+      if (pr < w.n_packed && (((again[x] | again[x] >> 32) >> r & 1 && has_hidden(w, G, pr)) || (empty[x] >> r & 1 && has_keys(w, G, pr)))) redo_row<BF16, HD>(a, w, kvh, G, pr);
     }
   }
 }
@@ -858,7 +867,7 @@ __global__ void __launch_bounds__(BLOCK) k_paged_attention_merge(PagedAttnArgs a
   for (int x = LANES; x < 64; x *= 2)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], x, WAVE);
-  o *= l == 0.f ? 0.f : 1.f / l;
+  o *= l == 0.f ? (__any(pm == -INFINITY) ? NAN : 0.f) : 1.f / l;
   if (sub) return;
   T* dst = (T*)a.out + (size_t)row * a.out_stride + head * HD + d;
   if constexpr (sizeof(T) == 2) *(uint2*)dst = make_uint2(f2_to_bf16x2(o[0], o[1]), f2_to_bf16x2(o[2], o[3]));

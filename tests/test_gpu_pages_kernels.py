@@ -214,3 +214,64 @@ def test_steps_of_a_served_batch_with_a_prefix_of_its_own(dtype, heads, bt, voic
     sh, _, parts_sh, parts = ssd.paged_attention_plan(pages, nq, n_seqs, n_seqs * 20 + 5, voice + 6 * bt, voice // bt)
     assert sh > 0 and parts_sh > 1 and parts > 1
     serve(dtype, heads, bt, voice, n_seqs=n_seqs, steps=5, graph=graph)
+
+
+@pytest.mark.parametrize("case", SMALLEST, ids=name)
+def test_kernel_and_scores_of_minus_infinity(case):
+    """A softmax whose scores are all -inf is NaN, as its formula is, and not the zeros of a row that has no position; with one finite score the others count for nothing."""
+    b = Planned(case)
+    b.q = b.q.abs() + 0.1
+    G, L = b.nq // b.nkv, [n + r for n, r in zip(b.lens, b.rows)]
+    keep = [torch.ones(n, dtype=torch.bool, device="cuda") for n in L]
+    nothing = torch.zeros((b.n, b.nq), dtype=torch.bool, device="cuda")
+
+    def low(s, positions):
+        blocks = torch.tensor([b.block(s, int(p) // b.bt) for p in positions], dtype=torch.int64, device="cuda")
+        b.keys[blocks, 0, positions.cuda() % b.bt, 1] = -math.inf
+        keep[s][positions.cuda()] = False
+
+    own = [b.sb * b.bt if b.sb and j else 0 for j in b.joins]
+    for i, s in enumerate(s for s, r in enumerate(b.rows) if r):
+        r = b.rows[s]
+        if i % 4 == 0:                                     # all that its first rows see of its own keys; without a prefix, all that they see
+            low(s, torch.arange(own[s], b.lens[s] + (r + 1) // 2))
+            if not own[s]:
+                nothing[b.start[s]:b.start[s] + (r + 1) // 2, :G] = True
+        elif i % 4 == 1:                                   # the first 64, 128, ..: whole chunks, and parts
+            low(s, torch.arange(own[s], own[s] + (b.lens[s] - own[s]) // 64 * 64))
+        elif i % 4 == 2:
+            low(s, torch.arange(own[s], L[s]))
+            if not own[s]:
+                nothing[b.start[s]:b.start[s + 1], :G] = True
+    for turn in range(2 if b.sb else 1):
+        if turn:                                           # and the whole prefix
+            at = torch.tensor(b.prefix, device="cuda")
+            b.keys[at, 0, :, 1] = -math.inf
+            for s, j in enumerate(b.joins):
+                if j:
+                    keep[s][:own[s]] = False
+                    seen = torch.arange(L[s], device="cuda") <= b.lens[s] + torch.arange(b.rows[s], device="cuda")[:, None]
+                    nothing[b.start[s]:b.start[s + 1], :G] = ~(keep[s] & seen).any(-1)[:, None]
+        out = b.run()
+        assert b.status == 0
+        assert torch.equal(torch.isnan(out).all(-1), nothing) and torch.equal(torch.isnan(out).any(-1), nothing)
+        for s, r in enumerate(b.rows):
+            if r:
+                at = slice(b.start[s], b.start[s + 1])
+                for heads, k in ((slice(0, G), keep[s]), (slice(G, None), None)):
+                    o, e = b.oracle(s, b.hd ** -0.5, k)
+                    assert bool((((out[at] - o).abs() <= e)[:, heads] | nothing[at, heads, None]).all()), (turn, s)
+    assert bool(nothing.any())
+
+
+def test_scores_near_the_lowest_number_count():
+    """fp32: scores of -2.2e38, and of that times log2(e) -3.2e38, are scores."""
+    b = Batch([(100, 1), (0, 1), (700, 9)], 4, 2, 64, 16, FP32, seed=2)
+    b.q[:], b.keys[:] = 0.0, 0.0
+    b.q[..., 0], b.keys[..., 0] = 1e19, -2.2e19
+    out = b.run(scale=1.0)
+    for s in range(3):
+        v = b.v[s].double().repeat_interleave(2, 1).cumsum(0)[b.lens[s]:]
+        n = torch.arange(b.lens[s] + 1, b.lens[s] + b.rows[s] + 1, device="cuda")[:, None, None]
+        size = b.v[s].double().abs().repeat_interleave(2, 1).cumsum(0)[b.lens[s]:] / n
+        assert bool(((out[b.start[s]:b.start[s + 1]].double() - v / n).abs() <= size * 2 * (700 + 64) * U32).all())
