@@ -53,6 +53,7 @@ struct PagedAttnArgs {
   int own_chunks;        // chunks of a part of a sequence's keys, at least
   int sh_slots, own_slots;             // tiles of query rows of the shared prefix, of the sequences: workgroups are sh_slots x P_sh x nkv and then own_slots x (P - P_sh) x nkv
 };
+static_assert(sizeof(PagedAttnArgs) % 4 == 0, "");
 
 struct SeqRows {
   int r0, n;             // first row of the launch, number of rows
@@ -174,6 +175,17 @@ __device__ __forceinline__ u32x4 factor_into(const PagedAttnArgs& a, u32x4 q, ui
 __device__ __forceinline__ bool has_hidden(const Work& w, int G, int pr) { return !w.shared && w.len + pr / G + 1 < w.k_end; }
 __device__ __forceinline__ bool has_keys(const Work& w, int G, int pr) { return w.shared || w.k_begin < w.len + pr / G + 1; }
 __device__ __forceinline__ bool all_finite(f32x4 v) { return v[0] * 0.f + v[1] * 0.f + v[2] * 0.f + v[3] * 0.f == 0.f; }
+// The arguments, read from where the launch put them: what only a row that is done over asks for is then in no register before that.  (With them in registers the loops over keys
+// have some of their own conditions and constants in vector registers: 1 % of a call's time.)
+__device__ __forceinline__ PagedAttnArgs args_again() {
+  typedef const __attribute__((address_space(4))) uint32_t* Words;
+  struct Copy { uint32_t w[sizeof(PagedAttnArgs) / 4]; } c;
+  Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(PagedAttnArgs) / 4); ++i) c.w[i] = p[i];
+  return __builtin_bit_cast(PagedAttnArgs, c);
+}
 template <typename DT, int HD>
 __device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, int kvh, int G, int pr) {
   typedef typename DT::T T;
@@ -424,7 +436,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
     if (more) load_values(base_next, k_next);
   }
   if (__any(bad) && lane == 0 && a.status) atomicOr(a.status, ST_PAGE);
-  uint32_t again = 0, empty = 0;                           // rows of which this lane has written something that is not finite; whose weights sum up to 0
+  uint32_t again = 0;                                      // rows of which this lane has written something that is to be done over
   float (*po)[16][HD + 4] = (float (*)[16][HD + 4])lds;
   float (*pm)[16] = (float (*)[16])(lds + 4 * 16 * (HD + 4)), (*pl)[16] = pm + 4;
 #pragma unroll
@@ -467,8 +479,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
         acc += *(const f32x4*)&po[y][r][d] * f;
       }
       const int pr = w.row0 + 16 * x + r, row = w.seq_r0 + pr / G, head = kvh * G + pr % G;
-      if (!SHARED && !all_finite(acc)) again |= 1u << (16 * x + r);
-      if (sum == 0.f) empty |= 1u << (16 * x + r);
+      if (!SHARED && !all_finite(acc) ? has_hidden(w, G, pr) : sum == 0.f && has_keys(w, G, pr)) again |= 1u << (16 * x + r);
       if (w.slot < 0) {
         T* dst = (T*)a.out + (size_t)row * a.out_stride + head * HD + d;
         acc *= sum == 0.f ? 0.f : 1.f / sum;
@@ -481,13 +492,12 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
       }
     }
   }
-  if (__any(again | empty)) {
+  if (__builtin_expect(__any(again), 0)) {                 // (or its code stands before the end that every call comes to)
     // (one wave has written the whole of a row; it writes it again behind that)
     __builtin_amdgcn_s_waitcnt(0x0070);
-    for (int r = 0; r < rows; ++r) {
-      const int pr = w.row0 + r;
-      if ((__any(again >> r & 1) && has_hidden(w, G, pr)) || (__any(empty >> r & 1) && has_keys(w, G, pr))) redo_row<DT, HD>(a, w, kvh, G, pr);
-    }
+    const PagedAttnArgs b = args_again();
+    for (int r = 0; r < rows; ++r)
+      if (__any(again >> r & 1)) redo_row<DT, HD>(b, w, kvh, G, w.row0 + r);
   }
 }
 
@@ -751,7 +761,6 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
         }
     }
   }
-  unsigned long long again[QS], empty[QS];                 // lanes that have written something that is not finite; whose rows' weights sum up to 0
 #pragma unroll
   for (int x = 0; x < QS; ++x) {
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[x]), __float_as_uint(l[x]), false, false);
@@ -761,35 +770,33 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
     for (int d = 0; d < J; ++d)
 #pragma unroll
       for (int e = 0; e < 4; ++e) any += f32x4{o[x][d][4 * e], o[x][d][4 * e + 1], o[x][d][4 * e + 2], o[x][d][4 * e + 3]} * 0.f;
-    again[x] = __ballot(!SHARED && !all_finite(any));
-    empty[x] = __ballot(ls == 0.f);
-    if (w0 + 32 * x + c >= w.n_packed) continue;
-    // dims 32 d + 8 e + 4 h .. + 3 in registers 4 e ..
-    if (w.slot < 0) {
-      const float inv = ls == 0.f ? 0.f : 1.f / ls;
-      bf16_t* dst = (bf16_t*)a.out + row[x] * a.out_stride + head[x] * HD + 4 * h;
+    const int pr = w0 + 32 * x + c;
+    const bool odd = !SHARED && !all_finite(any);
+    if (pr < w.n_packed) {
+      // dims 32 d + 8 e + 4 h .. + 3 in registers 4 e ..
+      if (w.slot < 0) {
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        bf16_t* dst = (bf16_t*)a.out + row[x] * a.out_stride + head[x] * HD + 4 * h;
 #pragma unroll
-      for (int d = 0; d < J; ++d)
+        for (int d = 0; d < J; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *(uint2*)(dst + 32 * d + 8 * e) = make_uint2(f2_to_bf16x2(o[x][d][4 * e] * inv, o[x][d][4 * e + 1] * inv), f2_to_bf16x2(o[x][d][4 * e + 2] * inv, o[x][d][4 * e + 3] * inv));
-    } else {
-      const size_t at = ((size_t)row[x] * a.nq + head[x]) * a.P + w.slot;
-      float* dst = a.o_part + at * HD + 4 * h;
+          for (int e = 0; e < 4; ++e)
+            *(uint2*)(dst + 32 * d + 8 * e) = make_uint2(f2_to_bf16x2(o[x][d][4 * e] * inv, o[x][d][4 * e + 1] * inv), f2_to_bf16x2(o[x][d][4 * e + 2] * inv, o[x][d][4 * e + 3] * inv));
+      } else {
+        const size_t at = ((size_t)row[x] * a.nq + head[x]) * a.P + w.slot;
+        float* dst = a.o_part + at * HD + 4 * h;
 #pragma unroll
-      for (int d = 0; d < J; ++d)
+        for (int d = 0; d < J; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *(f32x4*)(dst + 32 * d + 8 * e) = f32x4{o[x][d][4 * e], o[x][d][4 * e + 1], o[x][d][4 * e + 2], o[x][d][4 * e + 3]};
-      if (h == 0) { a.ml_part[at * 2] = m[x]; a.ml_part[at * 2 + 1] = ls; }
+          for (int e = 0; e < 4; ++e) *(f32x4*)(dst + 32 * d + 8 * e) = f32x4{o[x][d][4 * e], o[x][d][4 * e + 1], o[x][d][4 * e + 2], o[x][d][4 * e + 3]};
+        if (h == 0) { a.ml_part[at * 2] = m[x]; a.ml_part[at * 2 + 1] = ls; }
+      }
     }
-  }
-#pragma unroll
-  for (int x = 0; x < QS; ++x) {
-    if (!(again[x] | empty[x])) continue;
-    __builtin_amdgcn_s_waitcnt(0x0070);
-    for (int r = 0; r < 32; ++r) {
-      const int pr = w0 + 32 * x + r;
-      if (pr < w.n_packed && (((again[x] | again[x] >> 32) >> r & 1 && has_hidden(w, G, pr)) || (empty[x] >> r & 1 && has_keys(w, G, pr)))) redo_row<BF16, HD>(a, w, kvh, G, pr);
+    if (__builtin_expect(has_rows && __any(odd || ls == 0.f), 0)) {
+      __builtin_amdgcn_s_waitcnt(0x0070);
+      const PagedAttnArgs b = args_again();
+      const unsigned long long again = __ballot(pr < w.n_packed && (odd ? has_hidden(w, G, pr) : ls == 0.f && has_keys(w, G, pr)));
+      for (uint32_t rows = (uint32_t)(again | again >> 32); rows; rows &= rows - 1) redo_row<BF16, HD>(b, w, kvh, G, w0 + 32 * x + __builtin_ctz(rows));
     }
   }
 }
