@@ -270,7 +270,7 @@ int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads, const voi
  * dev_shared given, those of dev_shared[s] >= shared_blocks; others read all positions through their own table.  The prefix is read once for all
  * rows, not through the sequences' tables.  max_len: about the largest len + rows; it decides how the keys are cut, not what is read, and a
  * wrong one costs time only.  The result of a row depends on how its call is cut, by the rounding of sums in another order, and the same call gives the same
- * bits.  Sums and softmax are fp32; with bf16 pages the weights are rounded to bf16 for their product with the values.
+ * bits.  Sums and softmax are fp32 (a score whose product with log2(e) is beyond its range is an infinite one); with bf16 pages the weights are rounded to bf16 for their product with the values.
  *   A position whose block is not in the pool or not in the table is left out, and SSD_STATUS_PAGE ORed to dev_status[0] (may be null); a row that has
  * no position left gets zeros (one whose scores are all -inf NaN, as softmax has it).  What lies in positions that a row does not see, infinities and NaN too, does not reach it.
  *   dev_ws: ssd_paged_attention_workspace_bytes() is enough for every call over such pages and heads with no more sequences, rows, max_len and shared blocks (one workspace, sized for

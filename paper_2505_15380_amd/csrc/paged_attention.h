@@ -12,7 +12,8 @@
 // Scores and outputs are computed transposed (S^T = K Q^T, O^T = V^T P^T): a lane holds scores and outputs of one query row, the weights go from the
 // first product's accumulators into the second one without leaving the registers, and both operands come from the pages as 16 bytes per lane.
 // Weights are powers of two of scores less a reference, the largest score of the first keys, which moves only to one that exceeds it by
-// PA_LAZY: most steps need neither a maximum across lanes nor a scaling of what is summed.  A weight is then at most 2^8, and as exact.
+// PA_LAZY: most steps need neither a maximum across lanes nor a scaling of what is summed.  A weight is then at most 2^8, and as exact: the reference is that score rounded up, since a
+// weight takes its score unrounded, and from scores of 2^31 on half a step of a float would be more than a power of two can hold.
 // The bf16 kernels round the weights to bf16 for the second product (2^-9 of each on average, at random: the sum is off by about as much as the
 // output's own rounding).  Their sum is held in fp32: tiles take it of the rounded weights, by dot instructions, streams of the unrounded ones.
 //
@@ -34,6 +35,7 @@ constexpr int PA_WAVES = 4, PA_THREADS = PA_WAVES * WAVE;        // of a workgro
 constexpr int PA_CHUNK = 64;           // keys in which parts are counted
 constexpr float PA_LAZY = 8.0f, PA_LARGE = 256.0f;
 constexpr float PA_NONE = -3.402823466e38f;                      // the reference of a row that has seen nothing: no score that is a number is below it
+constexpr float PA_FAINT = 0x1p-60f;   // a sum of weights below this is one of weights that have run out, or of none: the largest is 1 less a few steps of its score
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 struct PagedAttnArgs {
@@ -163,6 +165,9 @@ __device__ __forceinline__ int checked_block(const PagedAttnArgs& a, const Work&
   return there ? blk : -1;
 }
 
+// No less than the product that `s` is rounded from.
+__device__ __forceinline__ float above(float s) { return fmaf(fabsf(s), 0x1p-23f, s); }
+
 // A negative factor leaves its sign with the queries, so that the largest product is the largest score; of 0 the queries become zeros (and a hidden
 // key's score stays -inf).
 __device__ __forceinline__ float factor(const PagedAttnArgs& a) { return a.scale2 == 0.f ? 1.f : fabsf(a.scale2); }
@@ -170,8 +175,8 @@ __device__ __forceinline__ u32x4 factor_into(const PagedAttnArgs& a, u32x4 q, ui
 
 // Rows that share a tile do not all see its last keys.  The weight of a hidden key is 0, and 0 times a value that is not finite is NaN, so a row with such a key and a result
 // that is not finite is done over, by one wave, from the keys that it sees: the products then need no look at the values, and this is as rare as infinities in a cache are.
-//   So is a row whose weights sum up to 0 although there are keys before it: its blocks are missing, or all of its scores are -inf, and a softmax of these is NaN. Of a part, the
-// reference -inf says so, and becomes NaN if no other part has anything.
+//   So is a row whose weights sum up to nothing although there are keys before it: its blocks are missing; its scores are so large that steps of a float decide (here they are rounded
+// before they are subtracted); or all of them are -inf, and a softmax of these is NaN. Of a part, the reference -inf says so, and becomes NaN if no other part has anything.
 __device__ __forceinline__ bool has_hidden(const Work& w, int G, int pr) { return !w.shared && w.len + pr / G + 1 < w.k_end; }
 __device__ __forceinline__ bool has_keys(const Work& w, int G, int pr) { return w.shared || w.k_begin < w.len + pr / G + 1; }
 __device__ __forceinline__ bool all_finite(f32x4 v) { return v[0] * 0.f + v[1] * 0.f + v[2] * 0.f + v[3] * 0.f == 0.f; }
@@ -399,7 +404,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
-      mx *= scale2;
+      mx = above(mx * scale2);
       if (__any(mx > m[x] + PA_LAZY)) {
         mx = max_over_groups(mx);
         if (mx > m[x] + PA_LAZY) {
@@ -479,7 +484,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
         acc += *(const f32x4*)&po[y][r][d] * f;
       }
       const int pr = w.row0 + 16 * x + r, row = w.seq_r0 + pr / G, head = kvh * G + pr % G;
-      if (!SHARED && !all_finite(acc) ? has_hidden(w, G, pr) : sum == 0.f && has_keys(w, G, pr)) again |= 1u << (16 * x + r);
+      if (!SHARED && !all_finite(acc) ? has_hidden(w, G, pr) : sum < PA_FAINT && has_keys(w, G, pr)) again |= 1u << (16 * x + r);
       if (w.slot < 0) {
         T* dst = (T*)a.out + (size_t)row * a.out_stride + head * HD + d;
         acc *= sum == 0.f ? 0.f : 1.f / sum;
@@ -673,7 +678,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[x][t][i]);
           const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-          mx = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * scale2;
+          mx = above(fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * scale2);
           if (mx > m[x]) {
             const float keep = __builtin_amdgcn_exp2f(m[x] - mx);
             m[x] = mx;
@@ -792,10 +797,10 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
         if (h == 0) { a.ml_part[at * 2] = m[x]; a.ml_part[at * 2 + 1] = ls; }
       }
     }
-    if (__builtin_expect(has_rows && __any(odd || ls == 0.f), 0)) {
+    if (__builtin_expect(has_rows && __any(odd || ls < PA_FAINT), 0)) {
       __builtin_amdgcn_s_waitcnt(0x0070);
       const PagedAttnArgs b = args_again();
-      const unsigned long long again = __ballot(pr < w.n_packed && (odd ? has_hidden(w, G, pr) : ls == 0.f && has_keys(w, G, pr)));
+      const unsigned long long again = __ballot(pr < w.n_packed && (odd ? has_hidden(w, G, pr) : ls < PA_FAINT && has_keys(w, G, pr)));
       for (uint32_t rows = (uint32_t)(again | again >> 32); rows; rows &= rows - 1) redo_row<BF16, HD>(b, w, kvh, G, w0 + 32 * x + __builtin_ctz(rows));
     }
   }

@@ -264,6 +264,36 @@ def test_kernel_and_scores_of_minus_infinity(case):
     assert bool(nothing.any())
 
 
+@pytest.mark.parametrize("spread", [1e7, 1e10, 1e31])
+@pytest.mark.parametrize("case", SMALLEST, ids=name)
+def test_kernel_and_scores_of_any_size(case, spread):
+    """Scores whose steps of 2^-24 are more than what a power of two can hold, and zeros among them: where the largest is apart from the next one by more than the roundings, its value is the
+    result.  A score: hd products and their sum, the factors: (hd + 6) u of `size`, twice as they may go apart, and twice again."""
+    b = Planned(case)
+    b.q = (b.q * spread).to(b.dtype)
+    b.keys[:, :, 1::2] = 0                                 # (every other position)
+    for s in range(len(b.rows)):
+        b.k[s][1::2] = 0
+    out = b.run()
+    assert b.status == 0 and bool(torch.isfinite(out).all())
+    G, clear_rows, rows = b.nq // b.nkv, 0, 0
+    for s, r in enumerate(b.rows):
+        if not r:
+            continue
+        q = b.q[b.start[s]:b.start[s + 1]].double().transpose(0, 1).contiguous()
+        k, v = (t.double().repeat_interleave(G, 1).transpose(0, 1).contiguous() for t in (b.k[s], b.v[s]))
+        hidden = torch.arange(k.shape[1], device="cuda") > b.lens[s] + torch.arange(r, device="cuda")[:, None]
+        w = (torch.bmm(q, k.transpose(1, 2).contiguous()) * b.hd ** -0.5).masked_fill(hidden, -math.inf)
+        size = torch.bmm(q.abs(), k.abs().transpose(1, 2).contiguous()).masked_fill(hidden, 0).amax(-1) * b.hd ** -0.5
+        top, at = torch.cat([w, torch.full_like(w[..., :1], -math.inf)], -1).topk(2, -1)
+        clear = (top[..., 0] - top[..., 1] > 4 * (b.hd + 6) * U32 * size + 200).transpose(0, 1)
+        want = torch.gather(v, 1, at[..., :1].clamp(max=k.shape[1] - 1).expand(-1, -1, b.hd)).transpose(0, 1)
+        got = out[b.start[s]:b.start[s + 1]].double()
+        assert bool(((got - want).abs() <= want.abs() * (2.1 * U16 if b.dtype == BF16 else 4 * U32))[clear].all()), s
+        clear_rows, rows = clear_rows + int(clear.sum()), rows + clear.numel()
+    assert clear_rows > 0.5 * rows
+
+
 def test_scores_near_the_lowest_number_count():
     """fp32: scores of -2.2e38, and of that times log2(e) -3.2e38, are scores."""
     b = Batch([(100, 1), (0, 1), (700, 9)], 4, 2, 64, 16, FP32, seed=2)
