@@ -169,7 +169,7 @@ __device__ __forceinline__ int checked_block(const PagedAttnArgs& a, const Work&
 __device__ __forceinline__ float above(float s) { return fmaf(fabsf(s), 0x1p-23f, s); }
 
 // A negative factor leaves its sign with the queries, so that the largest product is the largest score; of 0 the queries become zeros (and a hidden
-// key's score stays -inf).
+// key's score stays -inf), but for rows whose query is not finite, which are done over: 0 times that is NaN.
 __device__ __forceinline__ float factor(const PagedAttnArgs& a) { return a.scale2 == 0.f ? 1.f : fabsf(a.scale2); }
 __device__ __forceinline__ u32x4 factor_into(const PagedAttnArgs& a, u32x4 q, uint32_t signs) { return a.scale2 == 0.f ? u32x4{0, 0, 0, 0} : q ^ signs; }
 
@@ -192,12 +192,21 @@ __device__ __forceinline__ PagedAttnArgs args_again() {
   return __builtin_bit_cast(PagedAttnArgs, c);
 }
 template <typename DT, int HD>
+__device__ __forceinline__ bool odd_query(const PagedAttnArgs& a, const Work& w, int kvh, int G, int pr) {
+  const typename DT::T* q = (const typename DT::T*)a.q + (size_t)(w.seq_r0 + pr / G) * a.q_stride + (kvh * G + pr % G) * HD;
+  float x = 0.f;
+#pragma unroll 8
+  for (int d = 0; d < HD; ++d) x = fmaf(DT::ld(q + d), 0.f, x);
+  return x != 0.f;
+}
+template <typename DT, int HD>
 __device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, int kvh, int G, int pr) {
   typedef typename DT::T T;
   constexpr int D = HD < 64 ? 1 : HD / 64;
   const int lane = threadIdx.x & 63, dim = lane & (HD - 1), row = w.seq_r0 + pr / G, head = kvh * G + pr % G, end = w.shared ? w.k_end : min(w.len + pr / G + 1, w.k_end), tmask = a.p.bt - 1;
   const T* q = (const T*)a.q + (size_t)row * a.q_stride + head * HD;
   float acc[D] = {}, mx = PA_NONE, sum = 0.f;
+  const float first = a.scale2 == 0.f ? 0.f : 1.f, then = a.scale2 == 0.f ? 1.f : a.scale2;            // (of a factor of 0, as factor_into() has it)
   bool seen = false;
   for (int k0 = w.k_begin; k0 < end; k0 += 64) {
     const int key = k0 + lane;
@@ -210,8 +219,8 @@ __device__ __forceinline__ void redo_row(const PagedAttnArgs& a, const Work& w, 
       const T* kp = (const T*)a.p.keys + (((size_t)blk * a.p.nkv + kvh) * a.p.bt + (key & tmask)) * HD;
       float dot = 0.f;
 #pragma unroll 8
-      for (int d = 0; d < HD; ++d) dot = fmaf(DT::ld(q + d), DT::ld(kp + d), dot);
-      s = a.scale2 == 0.f ? 0.f : dot * a.scale2;
+      for (int d = 0; d < HD; ++d) dot = fmaf(DT::ld(q + d) * first, DT::ld(kp + d), dot);
+      s = dot * then;
     }
     const float m = wave_max(s);
     if (m > mx) {
@@ -497,10 +506,11 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
       }
     }
   }
-  if (__builtin_expect(__any(again), 0)) {                 // (or its code stands before the end that every call comes to)
+  if (__builtin_expect(__any(again) || a.scale2 == 0.f, 0)) {          // (or its code stands before the end that every call comes to)
     // (one wave has written the whole of a row; it writes it again behind that)
     __builtin_amdgcn_s_waitcnt(0x0070);
     const PagedAttnArgs b = args_again();
+    if (b.scale2 == 0.f && lane < rows && (lane & 15) * (HD / 4) / WAVE % W == wave && odd_query<DT, HD>(b, w, kvh, G, w.row0 + lane)) again |= 1u << lane;
     for (int r = 0; r < rows; ++r)
       if (__any(again >> r & 1)) redo_row<DT, HD>(b, w, kvh, G, w.row0 + r);
   }
@@ -797,10 +807,11 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
         if (h == 0) { a.ml_part[at * 2] = m[x]; a.ml_part[at * 2 + 1] = ls; }
       }
     }
-    if (__builtin_expect(has_rows && __any(odd || ls < PA_FAINT), 0)) {
+    if (__builtin_expect(has_rows && (__any(odd || ls < PA_FAINT) || a.scale2 == 0.f), 0)) {
       __builtin_amdgcn_s_waitcnt(0x0070);
       const PagedAttnArgs b = args_again();
-      const unsigned long long again = __ballot(pr < w.n_packed && (odd ? has_hidden(w, G, pr) : ls < PA_FAINT && has_keys(w, G, pr)));
+      const unsigned long long again = __ballot(pr < w.n_packed && ((odd ? has_hidden(w, G, pr) : ls < PA_FAINT && has_keys(w, G, pr)) ||
+                                                                    (b.scale2 == 0.f && odd_query<BF16, HD>(b, w, kvh, G, pr))));
       for (uint32_t rows = (uint32_t)(again | again >> 32); rows; rows &= rows - 1) redo_row<BF16, HD>(b, w, kvh, G, w0 + 32 * x + __builtin_ctz(rows));
     }
   }

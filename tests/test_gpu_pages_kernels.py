@@ -264,6 +264,35 @@ def test_kernel_and_scores_of_minus_infinity(case):
     assert bool(nothing.any())
 
 
+@pytest.mark.parametrize("case", SMALLEST, ids=name)
+def test_kernel_with_a_scale_of_zero(case):
+    """Every position counts alike, but 0 times what is not finite is NaN: rows that see such a key, and rows whose query is one."""
+    b = Planned(case)
+    G = b.nq // b.nkv
+    want = torch.zeros((b.n, b.nq), dtype=torch.bool, device="cuda")
+    with_rows = [s for s, r in enumerate(b.rows) if r]
+    for i, s in enumerate(with_rows):
+        n, r, last = b.lens[s], b.rows[s], b.nkv - 1
+        if i % 2 == 0:
+            at = n + r // 2
+            b.keys[b.block(s, at // b.bt), last, at % b.bt, 2] = math.inf if i % 4 else -math.inf
+            want[b.start[s] + r // 2:b.start[s + 1], b.nq - G:] = True
+        elif i % 4 == 1:
+            b.q[b.start[s], 0, 7] = math.inf
+            want[b.start[s], 0] = True
+        else:
+            b.q[b.start[s + 1] - 1, b.nq - 1, 7] = math.nan
+            want[b.start[s + 1] - 1, b.nq - 1] = True
+    out = b.run(scale=0.0)
+    assert b.status == 0
+    assert torch.equal(torch.isnan(out).all(-1), want) and torch.equal(~torch.isfinite(out).all(-1), want)
+    b.q = torch.nan_to_num(b.q, nan=0.0, posinf=0.0)       # (the oracle takes every score as 0)
+    for s in with_rows:
+        o, e = b.oracle(s, 0.0)
+        at = slice(b.start[s], b.start[s + 1])
+        assert bool((((out[at] - o).abs() <= e) | want[at, :, None]).all()), s
+
+
 @pytest.mark.parametrize("spread", [1e7, 1e10, 1e31])
 @pytest.mark.parametrize("case", SMALLEST, ids=name)
 def test_kernel_and_scores_of_any_size(case, spread):
