@@ -191,6 +191,21 @@ __device__ __forceinline__ PagedAttnArgs args_again() {
   for (int i = 0; i < (int)(sizeof(PagedAttnArgs) / 4); ++i) c.w[i] = p[i];
   return __builtin_bit_cast(PagedAttnArgs, c);
 }
+// A block is missing (a wave calls this; T: packed rows of a workgroup of the shared prefix, 0 of another one).  The prefix is read for all rows, also where none has it in front: then nothing is.
+__device__ __forceinline__ void report_pages(const Work& w, int T, int G) {
+  const PagedAttnArgs a = args_again();
+  const int lane = threadIdx.x & 63;
+  if (!a.status) return;
+  if (T) {
+    bool any = false;
+    for (int s = lane; s < a.n_seqs; s += 64) {
+      const SeqRows r = seq_rows(a, s);
+      any |= r.n > 0 && r.start > 0 && r.r0 * G < w.row0 + T && (r.r0 + r.n) * G > w.row0;
+    }
+    if (!__any(any)) return;
+  }
+  if (lane == 0) atomicOr(a.status, ST_PAGE);
+}
 template <typename DT, int HD>
 __device__ __forceinline__ bool odd_query(const PagedAttnArgs& a, const Work& w, int kvh, int G, int pr) {
   const typename DT::T* q = (const typename DT::T*)a.q + (size_t)(w.seq_r0 + pr / G) * a.q_stride + (kvh * G + pr % G) * HD;
@@ -449,7 +464,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
     }
     if (more) load_values(base_next, k_next);
   }
-  if (__any(bad) && lane == 0 && a.status) atomicOr(a.status, ST_PAGE);
+  if (__builtin_expect(__any(bad), 0)) report_pages(w, SHARED ? 16 * RT : 0, G);
   uint32_t again = 0;                                      // rows of which this lane has written something that is to be done over
   float (*po)[16][HD + 4] = (float (*)[16][HD + 4])lds;
   float (*pm)[16] = (float (*)[16])(lds + 4 * 16 * (HD + 4)), (*pl)[16] = pm + 4;
@@ -742,7 +757,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
         for (int x = 0; x < QS; ++x) o[x][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, p[x][k], o[x][d], 0, 0, 0);
       }
   }
-  if (__any(bad) && lane == 0 && a.status) atomicOr(a.status, ST_PAGE);
+  if (__builtin_expect(__any(bad), 0)) report_pages(w, SHARED ? T : 0, G);
   if constexpr (KW == 2) {
     // the second wave's references, sums and outputs: [wave][QS][4 J + 1][lane] of four
     static_assert(2 * QS * (4 * J + 1) * 64 <= 16 * J * 64, "");

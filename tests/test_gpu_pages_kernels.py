@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests.page_plans import BATCHES, BF16, FP32, KERNELS, name, ragged
-from tests.test_gpu_pages import U16, U32, Batch, serve
+from tests.test_gpu_pages import U16, U32, Batch, i32, serve
 
 pytestmark = pytest.mark.gpu
 
@@ -334,3 +334,20 @@ def test_scores_near_the_lowest_number_count():
         n = torch.arange(b.lens[s] + 1, b.lens[s] + b.rows[s] + 1, device="cuda")[:, None, None]
         size = b.v[s].double().abs().repeat_interleave(2, 1).cumsum(0)[b.lens[s]:] / n
         assert bool(((out[b.start[s]:b.start[s + 1]].double() - v / n).abs() <= size * 2 * (700 + 64) * U32).all())
+
+
+@pytest.mark.parametrize("case", [c for c in SMALLEST if c[1][5]], ids=name)
+def test_kernel_and_a_prefix_that_nobody_has(case):
+    """Blocks of the prefix that are not in the pool are reported if some row would read them, and not if no sequence has the prefix in front."""
+    (dtype, hd, *_), (nq, nkv, B, per, own, sb, bt, *_) = case
+    b = Planned(case)
+    b.joins = [False] * B
+    for s in range(B):                                     # through their own tables, all of them
+        if s % 5 != 4:
+            b.table[s, :sb] = torch.tensor(b.prefix)
+    b.prefix = [b.keys.shape[0] + i for i in range(sb)]
+    b.check(b.run(shared=i32([0] * B)))
+    assert b.status == 0
+    some = next(s for s, r in enumerate(b.rows) if r and s % 5 != 4)
+    b.run(shared=i32([sb if s == some else 0 for s in range(B)]))
+    assert b.status == 16
