@@ -246,7 +246,7 @@ typedef struct {
  * into dev_table (entries behind a sequence's blocks are left as they were), what was pushed into dev_free_stack, the new counts to dev_owned_out
  * [n_seqs] and dev_n_free_out [1] (which may be the input arrays), dev_row_start [n_seqs + 1] (row r of the step is one of s for row_start[s] <= r
  * < row_start[s + 1]) and of each row its sequence, position and slot, block * block_tokens + token, [max_rows] each; -1 for rows behind the
- * last.  dev_status[0] is set: 0, or SSD_STATUS_* bits, and then nothing has moved: tables, stack and counts are as before, row_start all 0 and
+ * last, and slot 2^31 - 1, which no pool has, for a row whose table entry is no block of the pool.  dev_status[0] is set: 0, or SSD_STATUS_* bits, and then nothing has moved: tables, stack and counts are as before, row_start all 0 and
  * rows -1, so that the calls below do nothing.  n_seqs <= 4096 (else SSD_ENOSUP).  dev_len and dev_rows are not changed. */
 int ssd_block_tables(int n_seqs, int block_tokens, int n_blocks, int table_cap, int max_rows, const int32_t* dev_len, const int32_t* dev_rows,
                      const int32_t* dev_shared, const int32_t* dev_owned, const int32_t* dev_n_free, int32_t* dev_table, int32_t* dev_free_stack,

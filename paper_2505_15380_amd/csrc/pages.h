@@ -91,8 +91,10 @@ __device__ __forceinline__ int owner_of(const int* ends, int B, int i) {
   return lo;
 }
 
+// (an id that is no block's, shifted, can be a slot of another block: it gets one that no pool has)
 __device__ __forceinline__ int slot_of(const BlockTableArgs& a, int seq, int pos) {
-  return (a.table[(size_t)seq * a.cap + (pos >> a.bt_shift)] << a.bt_shift) + (pos & ((1 << a.bt_shift) - 1));
+  const int blk = a.table[(size_t)seq * a.cap + (pos >> a.bt_shift)];
+  return (unsigned)blk < (unsigned)a.n_blocks ? (blk << a.bt_shift) + (pos & ((1 << a.bt_shift) - 1)) : 0x7FFFFFFF;
 }
 
 // The serial walk that the bookkeeping is defined by - sequences in ascending order give back what they no longer need, highest index first, then

@@ -351,3 +351,27 @@ def test_kernel_and_a_prefix_that_nobody_has(case):
     some = next(s for s, r in enumerate(b.rows) if r and s % 5 != 4)
     b.run(shared=i32([sb if s == some else 0 for s in range(B)]))
     assert b.status == 16
+
+
+@pytest.mark.parametrize("rows, bt", [(7, 16), (700, 64)])
+def test_a_table_of_blocks_outside_the_pool_reaches_no_slot(rows, bt):
+    """Ids that are no blocks, of which some shifted by the block size are slots of others: their rows get the slot 2^31 - 1, and an append leaves them out and says so."""
+    import paper_2505_15380_amd as ssd
+    wrong = [-1, 9, 1 << (32 - bt.bit_length() + 1), (1 << (32 - bt.bit_length() + 1)) + 3, -(1 << (32 - bt.bit_length() + 1)) + 2, 2 ** 31 - 1, -2 ** 31]
+    B, cap = len(wrong) + 1, -(-rows // bt) + 1
+    table = torch.full((B, cap), 0, dtype=torch.int32)
+    for s, x in enumerate(wrong):
+        table[s] = x
+    table[-1] = 5
+    owned = i32([cap] * B)
+    assert rows * B > 4096 or rows < 10                    # (looked up by one launch, and by two)
+    r = ssd.ssd_block_tables(i32([bt] * B), i32([min(rows, (cap - 1) * bt)] * B), bt, table.cuda(), owned, i32([0] * 9), i32([0]), rows * B)
+    n = min(rows, (cap - 1) * bt)
+    assert r["status"].item() == 0 and r["n_free"].item() == 0
+    slot = r["row_slot"][:n * B].view(B, n)
+    assert bool((slot[:-1] == 2 ** 31 - 1).all())
+    assert slot[-1].tolist() == [5 * bt + p % bt for p in range(bt, bt + n)]
+    keys, values = torch.zeros((9, 1, bt, 32), dtype=BF16, device="cuda"), torch.zeros((9, 1, 32, bt), dtype=BF16, device="cuda")
+    status, k = i32([0]), torch.ones((n * (B - 1), 1, 32), dtype=BF16, device="cuda")
+    ssd.ssd_rope_append(ssd.Pages(keys, values), r["row_pos"][:len(k)], r["row_slot"][:len(k)], k, k, status=status)
+    assert status.item() == 16 and not bool(keys.any()) and not bool(values.any())
