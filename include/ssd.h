@@ -231,7 +231,7 @@ int ssd_warp_probs(const float* dev_logits, int rows, int V, const ssd_sample_co
 
 /* One layer's pages, in the layout of ssd_kv's pool: keys [n_blocks][n_kv_heads][block_tokens][head_dim] after the rotary embedding, values
  * [n_blocks][n_kv_heads][head_dim][block_tokens], 16-byte aligned.  head_dim in {32,64,128}, block_tokens a power of two from 16 to 1024
- * (else SSD_ENOSUP); n_blocks * block_tokens < 2^31.  Positions that were never written may hold anything, NaN included. */
+ * (else SSD_ENOSUP); n_kv_heads <= 1024, n_blocks * block_tokens < 2^31.  Positions that were never written may hold anything, NaN included. */
 typedef struct {
   void*   dev_keys;
   void*   dev_values;
@@ -247,7 +247,7 @@ typedef struct {
  * [n_seqs] and dev_n_free_out [1] (which may be the input arrays), dev_row_start [n_seqs + 1] (row r of the step is one of s for row_start[s] <= r
  * < row_start[s + 1]) and of each row its sequence, position and slot, block * block_tokens + token, [max_rows] each; -1 for rows behind the
  * last, and slot 2^31 - 1, which no pool has, for a row whose table entry is no block of the pool.  dev_status[0] is set: 0, or SSD_STATUS_* bits, and then nothing has moved: tables, stack and counts are as before, row_start all 0 and
- * rows -1, so that the calls below do nothing.  n_seqs <= 4096 (else SSD_ENOSUP).  dev_len and dev_rows are not changed. */
+ * rows -1, so that the calls below do nothing.  n_seqs <= 4096, table_cap * block_tokens and max_rows <= 2^30 (else SSD_ENOSUP).  dev_len and dev_rows are not changed. */
 int ssd_block_tables(int n_seqs, int block_tokens, int n_blocks, int table_cap, int max_rows, const int32_t* dev_len, const int32_t* dev_rows,
                      const int32_t* dev_shared, const int32_t* dev_owned, const int32_t* dev_n_free, int32_t* dev_table, int32_t* dev_free_stack,
                      int32_t* dev_owned_out, int32_t* dev_n_free_out, int32_t* dev_row_start, int32_t* dev_row_seq, int32_t* dev_row_pos,
@@ -259,7 +259,7 @@ int ssd_block_tables(int n_seqs, int block_tokens, int n_blocks, int table_cap, 
  * head_dim behind each other, `stride` elements from row to row (columns of one QKV product as well), beginning at multiples of 16 bytes.
  * n_q_heads 0: keys and values alone.  A row with a negative position is left out, one with a negative slot is not appended; a slot outside the pool
  * or a position outside dev_rope is left out and ORed to dev_status[0] (may be null).  Slots >= 0 are distinct: of two rows with one slot either
- * may win, element by element. */
+ * may win, element by element.  n_rows <= 2^24, n_q_heads <= 1024; a launch of 2^32 threads or more is refused (SSD_ENOSUP), here and below. */
 int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads, const void* dev_q, size_t q_stride, const void* dev_k, size_t k_stride,
                     const void* dev_v, size_t v_stride, const float* dev_rope, int rope_positions, const int32_t* dev_row_pos,
                     const int32_t* dev_row_slot, void* dev_q_out, size_t q_out_stride, int32_t* dev_status, void* stream);
@@ -275,7 +275,7 @@ int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads, const voi
  * no position left gets zeros (one whose scores are all -inf NaN, as softmax has it).  What lies in positions that a row does not see, infinities and NaN too, does not reach it.
  *   dev_ws: ssd_paged_attention_workspace_bytes() is enough for every call over such pages and heads with no more sequences, rows, max_len and shared blocks (one workspace, sized for
  * the largest step, does for all of them); it may be 0 (dev_ws may be null then), and is (size_t)-1 for arguments that the call refuses.  A call itself asks for
- * n_rows * n_q_heads * parts * (head_dim + 2) floats if it is cut into parts (ssd_paged_attention_plan).  Calls that may overlap need workspaces of their own.  n_rows * n_q_heads <= 2^26, n_seqs <= 65536, table_cap * block_tokens <= 2^30. */
+ * n_rows * n_q_heads * parts * (head_dim + 2) floats if it is cut into parts (ssd_paged_attention_plan).  Calls that may overlap need workspaces of their own.  n_rows * n_q_heads <= 2^26, n_q_heads <= 1024, n_seqs <= 65536, table_cap * block_tokens <= 2^30. */
 size_t ssd_paged_attention_workspace_bytes(const ssd_pages* pages, int n_q_heads, int n_seqs, int n_rows, int max_len, int shared_blocks);
 int ssd_paged_attention(const ssd_pages* pages, int n_q_heads, float scale, int n_seqs, int n_rows, int max_len, const int32_t* dev_len,
                         const int32_t* dev_row_start, const int32_t* dev_table, int table_cap, int shared_blocks, const int32_t* dev_shared_table,

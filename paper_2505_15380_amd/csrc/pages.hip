@@ -16,6 +16,8 @@ using namespace ssd;
 
 static_assert(ST_POOL == SSD_STATUS_POOL && ST_TABLE == SSD_STATUS_TABLE && ST_ROWS == SSD_STATUS_ROWS && ST_BAD == SSD_STATUS_BATCH && ST_PAGE == SSD_STATUS_PAGE, "");
 
+constexpr long long MOST_THREADS = 0xFFFFFFFFll;           // of a launch
+
 static inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 static int log2_of(int v) {
   int s = 0;
@@ -96,7 +98,9 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
   const int per16 = pages->dtype == SSD_DTYPE_BF16 ? 8 : 4;
   const int v_wgs = cdiv(n_rows, RA_WINDOW) * a.p.nkv;
   const long long threads = (long long)n_rows * (a.p.hd / 2 / per16) * cdiv(n_q_heads + a.p.nkv, RA_HEADS);
-  const dim3 grid((unsigned)(v_wgs + (threads + BLOCK - 1) / BLOCK));
+  const long long wgs = v_wgs + (threads + BLOCK - 1) / BLOCK;
+  if (wgs > MOST_THREADS / BLOCK) return fail(SSD_ENOSUP, "n_rows = %d: more threads than a launch has", n_rows);
+  const dim3 grid((unsigned)wgs);
   if (pages->dtype == SSD_DTYPE_BF16) hipLaunchKernelGGL(k_rope_append<BF16>, grid, dim3(BLOCK), 0, (hipStream_t)stream, a, v_wgs);
   else hipLaunchKernelGGL(k_rope_append<F32>, grid, dim3(BLOCK), 0, (hipStream_t)stream, a, v_wgs);
   LAUNCH_CHECK();
@@ -244,7 +248,7 @@ extern "C" int ssd_paged_attention_plan(const ssd_pages* pages, int n_q_heads, i
 template <typename DT, int HD, int SH, int OWN>
 static int launch_attention(const PagedAttnArgs& a, hipStream_t st) {
   const long long wgs = ((long long)a.sh_slots * a.P_sh + (long long)a.own_slots * (a.P - a.P_sh)) * a.p.nkv;
-  if (wgs > 0x7FFFFFFFll) return fail(SSD_ENOSUP, "too many workgroups");
+  if (wgs > MOST_THREADS / PagedShape<SH, OWN>::THREADS || (a.P > 1 && (long long)a.n_rows * a.nq > MOST_THREADS / WAVE)) return fail(SSD_ENOSUP, "more threads than a launch has");
   hipLaunchKernelGGL((k_paged_attention<DT, HD, SH, OWN>), dim3((unsigned)wgs), dim3(PagedShape<SH, OWN>::THREADS), 0, st, a);
   LAUNCH_CHECK();
   if (a.P > 1) {

@@ -104,3 +104,12 @@ def test_the_binding_refuses_what_it_can_see():
             pg.rows("k", bad, 2)
     with pytest.raises(ssd.SSDError):                      # not on a GPU
         ssd.ssd_rope_append(pg, torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), rows, rows)
+
+
+def test_launches_of_more_threads_than_a_grid_has_are_refused(lib):
+    """2^32 threads and more; workgroups have 256, or 512."""
+    many = pages(n_kv_heads=1024)
+    assert lib.ssd_rope_append(*{**APPEND, "pages": C.byref(many), "n_rows": 1 << 24, "ks": 1 << 16, "vs": 1 << 16, "qs": 1 << 16, "os": 1 << 16}.values()) == ENOSUP
+    args = {**ATTEND, "pages": C.byref(many), "nq": 1024, "qs": 1 << 16, "os": 1 << 16, "shared_blocks": 0, "n_seqs": 1 << 16, "n_rows": 1 << 16}
+    assert lib.ssd_paged_attention(*args.values()) == ENOSUP
+    assert lib.ssd_last_error()
