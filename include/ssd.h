@@ -272,7 +272,8 @@ int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads, const voi
  * wrong one costs time only.  The result of a row depends on how its call is cut, by the rounding of sums in another order, and the same call gives the same
  * bits.  Sums and softmax are fp32 (a score whose product with log2(e) is beyond its range is an infinite one); with bf16 pages the weights are rounded to bf16 for their product with the values.
  *   A position whose block is not in the pool or not in the table is left out, and SSD_STATUS_PAGE ORed to dev_status[0] (may be null); a row that has
- * no position left gets zeros (one whose scores are all -inf NaN, as softmax has it).  What lies in positions that a row does not see, infinities and NaN too, does not reach it.
+ * no position left gets zeros (one whose scores are all -inf NaN, as softmax has it); the rows of a sequence whose length
+ * cannot be (negative, or longer than its table: SSD_STATUS_BATCH) are not written.  What lies in positions that a row does not see, infinities and NaN too, does not reach it.
  *   dev_ws: ssd_paged_attention_workspace_bytes() is enough for every call over such pages and heads with no more sequences, rows, max_len and shared blocks (one workspace, sized for
  * the largest step, does for all of them); it may be 0 (dev_ws may be null then), and is (size_t)-1 for arguments that the call refuses.  A call itself asks for
  * n_rows * n_q_heads * parts * (head_dim + 2) floats if it is cut into parts (ssd_paged_attention_plan).  Calls that may overlap need workspaces of their own.  n_rows * n_q_heads <= 2^26, n_q_heads <= 1024, n_seqs <= 65536, table_cap * block_tokens <= 2^30. */

@@ -375,3 +375,71 @@ def test_a_table_of_blocks_outside_the_pool_reaches_no_slot(rows, bt):
     status, k = i32([0]), torch.ones((n * (B - 1), 1, 32), dtype=BF16, device="cuda")
     ssd.ssd_rope_append(ssd.Pages(keys, values), r["row_pos"][:len(k)], r["row_slot"][:len(k)], k, k, status=status)
     assert status.item() == 16 and not bool(keys.any()) and not bool(values.any())
+
+
+@pytest.mark.parametrize("change, bit", [("pool", 1), ("table", 2), ("rows", 4), ("len", 8), ("over", 8)])
+def test_block_tables_of_many_rows_move_nothing_when_they_cannot(change, bit):
+    """More rows than the one workgroup looks up itself: the launch behind it leaves none either."""
+    import paper_2505_15380_amd as ssd
+    bt, B, cap, n_blocks, max_rows = 16, 40, 30, 700, 6000
+    lens, rows, owned, n_free = [20] * B, [140] * B, [2] * B, 600
+    if change == "pool": n_free = 300
+    if change == "table": lens[7] = cap * bt - 139
+    if change == "rows": rows[3] = 600
+    if change == "len": lens[39] = -1
+    if change == "over": lens[0], rows[0], owned[0], n_free = 0, 0, 30, 690
+    if change == "rows": cap = 60
+    d = dict(table=(torch.arange(B * cap, dtype=torch.int32) % n_blocks).view(B, cap).cuda(), owned=i32(owned), free_stack=torch.arange(n_blocks, dtype=torch.int32).cuda(), n_free=i32([n_free]))
+    kept = {k: v.clone() for k, v in d.items()}
+    r = ssd.ssd_block_tables(i32(lens), i32(rows), bt, d["table"], d["owned"], d["free_stack"], d["n_free"], max_rows)
+    assert r["status"].item() & bit
+    for k, v in d.items():
+        assert torch.equal(v, kept[k]), k
+    assert torch.equal(r["owned"], kept["owned"]) and torch.equal(r["n_free"], kept["n_free"]) and not bool(r["row_start"].any())
+    for k in ("row_seq", "row_pos", "row_slot"):
+        assert bool((r[k] == -1).all())
+
+
+def test_steps_without_rows():
+    """Nothing is written and nothing asked for."""
+    import paper_2505_15380_amd as ssd
+    b = Batch([(40, 0), (7, 0)], 4, 2, 64, 16, BF16, seed=1, shared_blocks=1)
+    pages, before = ssd.Pages(b.keys, b.values), b.keys.nan_to_num().clone()
+    none = torch.empty((0, 4, 64), dtype=BF16, device="cuda")
+    assert ssd.ssd_paged_attention(pages, none, i32(b.lens), i32([0, 0, 0]), i32(b.table), shared_table=i32(b.prefix)).shape == none.shape
+    assert ssd.ssd_rope_append(pages, i32([]), i32([]), none[:, :2], none[:, :2], q=none).shape == none.shape
+    padded = torch.full((5, 4, 64), 7.0, dtype=BF16, device="cuda")           # rows of the launch, of which no sequence has one
+    out = padded.clone()
+    ssd.ssd_paged_attention(pages, padded, i32(b.lens), i32([0, 0, 0]), i32(b.table), shared_table=i32(b.prefix), out=out, max_len=5000)
+    assert torch.equal(out, padded) and torch.equal(b.keys.nan_to_num(), before)
+    r = ssd.ssd_block_tables(i32(b.lens), i32([0, 0]), 16, torch.zeros((2, 9), dtype=torch.int32, device="cuda"), i32([4, 1]), i32([0] * 9), i32([2]), 3)
+    assert r["status"].item() == 0 and r["row_start"].tolist() == [0, 0, 0] and r["row_slot"].tolist() == [-1] * 3 and r["owned"].tolist() == [4, 2]
+
+
+@pytest.mark.parametrize("seqs, sb, hd", [([(50, 100), (700, 90)], 0, 128), ([(900, 700), (30, 900), (0, 800)], 0, 128), ([(n, 3) for n in range(30)], 60, 64),
+                                          ([(n * 30, 1) for n in range(8)], 0, 32)])
+def test_attention_and_append_over_a_pool_of_more_than_2_31_elements(seqs, sb, hd):
+    """Tiles, streams and a prefix in blocks far apart; a third of the blocks are the pool's last."""
+    import paper_2505_15380_amd as ssd
+    bt, nkv = 16, 2
+    n_blocks = (1 << 31) // (nkv * bt * hd) + 5000
+    b = Batch(seqs, 4, nkv, hd, bt, BF16, seed=hd + sb, shared_blocks=sb, n_blocks=n_blocks)
+    last = n_blocks - 1
+    for s, r in enumerate(b.rows):                         # some of every sequence's blocks move to the end
+        for i in range(sb, int((b.table[s] >= 0).sum()) + sb, 3):
+            old = int(b.table[s, i])
+            if old < 0 or last in (old, *b.prefix) or bool((b.table == last).any()):
+                continue
+            b.keys[last], b.values[last] = b.keys[old], b.values[old]
+            b.table[s, i] = last
+            last -= 1
+    assert last < n_blocks - 3 and (last + 1) * nkv * bt * hd > 1 << 31
+    b.check(b.run())
+    assert b.status == 0
+    rows = torch.randn((40, nkv, hd), device="cuda").to(BF16)
+    slot = torch.arange(40) + (n_blocks - 3) * bt
+    ssd.ssd_rope_append(ssd.Pages(b.keys, b.values), i32(list(range(40))), i32(slot), rows, rows)
+    blk, tok = slot.cuda() // bt, slot.cuda() % bt
+    assert torch.equal(b.keys[blk, :, tok], rows) and torch.equal(b.values[blk, :, :, tok], rows)
+    del b
+    torch.cuda.empty_cache()
