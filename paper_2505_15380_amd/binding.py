@@ -1,6 +1,7 @@
 """ctypes binding of libssd.so (include/ssd.h).  Argument marshalling only."""
 import ctypes as C
 import os
+import threading
 
 import numpy as np
 import torch
@@ -102,7 +103,7 @@ def load_library():
         "ssd_paged_attention_workspace_bytes": (sz, [C.POINTER(_Pages), i32, i32, i32, i32, i32]),
         "ssd_paged_attention": (i32, [C.POINTER(_Pages), i32, C.c_float, i32, i32, i32, i32p, i32p, i32p, i32, i32, i32p, i32p, vp, sz, vp, sz,
                                       vp, sz, i32p, vp]),
-        "ssd_paged_attention_plan": (i32, [C.POINTER(_Pages), i32, i32, i32, i32, i32, C.POINTER(C.c_int)]),
+        "ssd_paged_attention_plan": (i32, [C.POINTER(_Pages), i32, i32, i32, i32, i32, vp]),
         "ssd_strerror": (C.c_char_p, [i32]),
         "ssd_last_error": (C.c_char_p, []),
     }
@@ -433,6 +434,17 @@ class Pages:
         return st[0] if sh[0] > 1 else heads * hd
 
 
+class _Plan(threading.local):
+    """Where a thread's plans go: a new array for each costs a call 1 us."""
+
+    def __init__(self):
+        self.of = (C.c_int * 4)()
+        self.address = C.addressof(self.of)
+
+
+_plan = _Plan()
+
+
 def ssd_block_tables(lens, rows, block_tokens, table, owned, free_stack, n_free, max_rows, shared=None, out=None):
     """Blocks and slots of a step.  lens, rows, owned[, shared] [n_seqs], table [n_seqs, cap], free_stack [n_blocks], n_free [1]: int32 device
     tensors; table and free_stack are written.  Returns dict(owned, n_free, row_start [n_seqs + 1], row_seq, row_pos, row_slot [max_rows],
@@ -487,7 +499,10 @@ def ssd_paged_attention(pages, q, lens, row_start, table, scale=None, shared_tab
     if max_len is None:
         max_len = cap * pages.block_tokens
     if ws is None:
-        parts = paged_attention_plan(pages, nq, B, n, max_len, sb)[3] if n else 1
+        parts = 1
+        if n:
+            _check(load_library().ssd_paged_attention_plan(pages.ref, nq, B, n, max_len, sb, _plan.address))
+            parts = _plan.of[3]
         ws = torch.empty(n * nq * parts * (hd + 2) * 4, dtype=torch.uint8, device=q.device) if parts > 1 else None
     elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
         raise SSDError(-1, "ws is a uint8 tensor in one piece on the device of the pages")
@@ -508,9 +523,8 @@ def paged_attention_workspace(pages, n_q_heads, n_seqs, n_rows, max_len, shared_
 
 def paged_attention_plan(pages, n_q_heads, n_seqs, n_rows, max_len, shared_blocks=0):
     """What ssd_paged_attention runs for such a call: (kind of the shared prefix's workgroups, kind of the sequences' own, parts of the prefix, parts of a row)."""
-    plan = (C.c_int * 4)()
-    _check(load_library().ssd_paged_attention_plan(pages.ref, n_q_heads, n_seqs, n_rows, max_len, shared_blocks, plan))
-    return tuple(plan)
+    _check(load_library().ssd_paged_attention_plan(pages.ref, n_q_heads, n_seqs, n_rows, max_len, shared_blocks, _plan.address))
+    return tuple(_plan.of)
 
 
 PROFILE_KINDS = {"qkv": 0, "attention": 1, "o": 2, "gate_up": 3, "down": 4, "head": 5, "persistent": 6}
