@@ -14,15 +14,17 @@
 // Weights are powers of two of scores less a reference, the largest score of the first keys, which moves only to one that exceeds it by
 // PA_LAZY: most steps need neither a maximum across lanes nor a scaling of what is summed.  A weight is then at most 2^8, and as exact: the reference is that score rounded up, since a
 // weight takes its score unrounded, and from scores of 2^31 on half a step of a float would be more than a power of two can hold.
-// The bf16 kernels round the weights to bf16 for the second product (2^-9 of each on average, at random: the sum is off by about as much as the
-// output's own rounding).  Their sum is held in fp32: tiles take it of the rounded weights, by dot instructions, streams of the unrounded ones.
+// The bf16 kernels round the weights to bf16 for the second product (2^-9 of each on average, at random): the error is 0.0022 of the result's norm, where the output's own rounding alone
+// leaves 0.0017.  With a second product of what the rounding drops it is 0.0017 too, but that is 8 % of the time in the mean over 27 calls, 37 % of 256 x 5 rows behind 16384 positions and 44 %
+// of prompts (62.6 -> 90.0 us).  Their sum is held in fp32: tiles take it of the rounded weights, by dot instructions, streams of the unrounded ones.
 //
 // What bounds a call (0.5B heads, 14 x 64 over 2, bf16, one MI355X; kernel times):
 //   few rows      the dependent steps - lengths, table, keys, scores, values, LDS - of which one token over 1024 positions takes 8.3 us; 16 x 7 rows over 256 to 4096 positions 11.5
-//                 us and 4.0 for the merge, where the bytes would take 3.1
-//   a prefix      of 16384 positions for 256 x 5 rows: 96 us, 790 TFLOP/s; the matrix units are busy for 35 % of that, the vector units (weights: a power of two, a product, half a
-//                 conversion and half a sum each) for 45 %, and two waves of a SIMD hardly overlap the one with the other
-//   prompts       seven of 100 to 2001 rows behind 1024 positions: 68 us, 650 TFLOP/s, 28 and 38 %: the same, and compute units with more workgroups than others
+//                 us and 3.9 for the merge, where the bytes would take 3.1
+//   a prefix      of 16384 positions for 256 x 5 rows: 96 to 103 us, 740 to 790 TFLOP/s; the matrix units are busy for 34 % of that, the vector units (weights: a power of two, a product, half a
+//                 conversion and half a sum each) for 44 %, and two waves of a SIMD hardly overlap the one with the other
+//   prompts       seven of 100 to 2001 rows behind 1024 positions: 68 to 70 us, 650 TFLOP/s, 28 and 39 %: the same, and compute units with more workgroups than others
+//   what is not finite   a row that is done over takes one wave for its keys, a row at a time: seven such prompts with a NaN in every block 28 ms, 16 x 7 rows 1.2 ms
 #pragma once
 #include <type_traits>
 

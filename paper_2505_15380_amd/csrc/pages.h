@@ -100,9 +100,10 @@ __device__ __forceinline__ int slot_of(const BlockTableArgs& a, int seq, int pos
 // The serial walk that the bookkeeping is defined by - sequences in ascending order give back what they no longer need, highest index first, then
 // in ascending order take what they lack - as prefix sums: they say where on the stack each sequence's blocks go and come from.  One workgroup:
 // what it puts on the stack it takes from there again behind a barrier.
-//   Bound by latency: eight dependent steps of memory, LDS and barriers are 4.4 us for 64 sequences of a row, whose 3 KB are nothing; 960
+//   Bound by latency: eight dependent steps of memory, LDS and barriers are 4.5 us for 64 sequences of a row, whose 3 KB are nothing; 960
 // sequences that move 8000 ids and look 76000 rows up: 14 us, and 4 for the rows' own launch, where the megabyte would take 0.2.  Which sequence an entry is of is searched
-// for in LDS; steps of a fixed number, several searches side by side, came to 14.8.  Parts of the walk on several workgroups would be three launches, 13 us by their parts.
+// for in LDS; steps of a fixed number, several searches side by side, came to 14.8.  The walk's parts on several workgroups, which could look the rows up as well, are estimated at three launches of 13 us in
+// all against these 18; one workgroup was kept for the few sequences of most steps, and nothing else was built.
 __global__ void __launch_bounds__(BT_THREADS) k_block_tables(BlockTableArgs a) {
   __shared__ int gave[BT_MAX_SEQS], took[BT_MAX_SEQS], rowed[BT_MAX_SEQS];
   __shared__ unsigned long long w[48];
@@ -244,8 +245,9 @@ struct Unit<F32> {
 //   Values lie [dim][token], and a row brings one token of every dim: a workgroup takes 32 rows of a head through LDS and writes, for each dim, the
 // eight tokens of an aligned piece at once (16 bytes; fp32 32) where eight rows behind each other fill one, the piece of a row being the business
 // of the workgroup that has its first row; what fills no piece goes element by element.
-//   Bound by being a launch for small calls (112 rows of the 0.5B heads 5.0 us, 517 of four fp32 heads of 32 4.4) and by memory for long ones: 4099 rows of the 1.5B heads bring and take
-// 36 MB, 11.1 us = 3.2 TB/s, where a copy of that size reaches 4.7.  (Values a row at a time, 2 bytes to a line: 17.9; windows of 64 rows, heads one by one: 13.4.)
+//   Bound by being a launch for small calls (112 rows of the 0.5B heads 5.0 us, 517 of four fp32 heads of 32 4.4).  4099 rows of the 1.5B heads bring and take
+// 36 MB in 11.1 us, 3.2 TB/s, where a copy of that size would take 7.5: in the workgroups that put values, of the eight lanes whose rows fill a piece one writes it.  (Values a row at a time, 2 bytes to a
+// line: 17.9; windows of 64 rows, heads one by one: 13.4.)
 template <typename DT>
 __global__ void __launch_bounds__(BLOCK) k_rope_append(RopeAppendArgs a, int v_wgs) {
   typedef typename DT::T T;

@@ -112,8 +112,10 @@ extern "C" int ssd_rope_append(const ssd_pages* pages, int n_rows, int n_q_heads
 // the least estimated time,
 //     sqrt(longest^2 + load^2) + (3.8 + 0.195 per MB of results for each part, if there are several)  us and what every call takes,
 // `longest`: of the workgroups, alone on a compute unit; `load`: of all of them, spread over 256 compute units.  The terms were fitted to 7100 cuts of 126 calls (1 to 256 sequences,
-// 1 to 7600 rows, 9 to 16888 positions), but for the 3.8, of which a graph takes 2.3 and a launch by itself more.  The cut that is picked takes 5 % more time
-// in the mean than the best that was measured, and at most 25 %; rules on the rows of a sequence took 24 %, and up to three times.
+// 1 to 7600 rows, 9 to 16888 positions; bf16 heads of 64 and 128, fp32 heads of 32, with kernels that were up to 8 % slower in some calls), but for the 3.8, of which a graph takes 2.3 and a launch by
+// itself more, and for what bf16 heads of 32 and fp32 heads of 64 and 128 have of their own, which were fitted to nothing.  Of 348 other calls with the present kernels (9887 cuts,
+// profiles/cuts_paged_attention.txt) the cut that is picked takes 3.0, 2.9 and 4.8 % more time in the mean than the best that was measured with bf16 heads of 32, 64 and 128, and at most 1.38 times
+// as long; 7.8, 9.5 and 7.1 % with fp32 ones, and at most 1.73 times.  Rules on the rows of a sequence, measured on the 126, took 24 %, and up to three times.
 //   What the parts leave for the merge takes no more than a workspace that grows with rows, length and prefix, so that one for a caller's largest call does for every smaller one:
 // rows x heads x parts stay below twice the rows x heads (a shared prefix and own keys) + 2^18, which is 1024 workgroups of 256 rows.  Of 300000 sizes, up to 65536 rows and 512 heads, it
 // changes the cut of 1.4 %; by the estimate the mean call then takes 0.03 % longer, and the worst 11 %.
