@@ -208,6 +208,15 @@ __device__ __forceinline__ void report_pages(const Work& w, int T, int G) {
   }
   if (lane == 0) atomicOr(a.status, ST_PAGE);
 }
+// Is any block of the workgroup's keys in the pool?  (Without one, as of a prefix that is not there yet, all rows are zeros as they stand: asked once, not of each row.  A wave calls it.)
+__device__ __forceinline__ bool any_block(const PagedAttnArgs& a, const Work& w) {
+  bool any = false;
+  for (int k = w.k_begin & ~(a.p.bt - 1); k < w.k_end && !any; k += 64 << a.p.bt_shift) {
+    const int blk = block_of(a, w, k + ((threadIdx.x & 63) << a.p.bt_shift));
+    any = __any(blk >= 0 && blk < a.p.n_blocks);
+  }
+  return any;
+}
 template <typename DT, int HD>
 __device__ __forceinline__ bool odd_query(const PagedAttnArgs& a, const Work& w, int kvh, int G, int pr) {
   const typename DT::T* q = (const typename DT::T*)a.q + (size_t)(w.seq_r0 + pr / G) * a.q_stride + (kvh * G + pr % G) * HD;
@@ -527,6 +536,7 @@ __device__ __forceinline__ void paged_stream(const PagedAttnArgs& a, int id, flo
     // (one wave has written the whole of a row; it writes it again behind that)
     __builtin_amdgcn_s_waitcnt(0x0070);
     const PagedAttnArgs b = args_again();
+    if (!any_block(b, w)) return;
     if (b.scale2 == 0.f && lane < rows && (lane & 15) * (HD / 4) / WAVE % W == wave && odd_query<DT, HD>(b, w, kvh, G, w.row0 + lane)) again |= 1u << lane;
     for (int r = 0; r < rows; ++r)
       if (__any(again >> r & 1)) redo_row<DT, HD>(b, w, kvh, G, w.row0 + r);
@@ -827,6 +837,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
     if (__builtin_expect(has_rows && (__any(odd || ls < PA_FAINT) || a.scale2 == 0.f), 0)) {
       __builtin_amdgcn_s_waitcnt(0x0070);
       const PagedAttnArgs b = args_again();
+      if (!any_block(b, w)) return;
       const unsigned long long again = __ballot(pr < w.n_packed && ((odd ? has_hidden(w, G, pr) : ls < PA_FAINT && has_keys(w, G, pr)) ||
                                                                     (b.scale2 == 0.f && odd_query<BF16, HD>(b, w, kvh, G, pr))));
       for (uint32_t rows = (uint32_t)(again | again >> 32); rows; rows &= rows - 1) redo_row<BF16, HD>(b, w, kvh, G, w0 + 32 * x + __builtin_ctz(rows));

@@ -443,3 +443,30 @@ def test_attention_and_append_over_a_pool_of_more_than_2_31_elements(seqs, sb, h
     assert torch.equal(b.keys[blk, :, tok], rows) and torch.equal(b.values[blk, :, :, tok], rows)
     del b
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("bt", [16, 64, 256, 1024])
+@pytest.mark.parametrize("which", [0, 1, -1])
+def test_one_block_of_a_sequence_is_there(dtype, bt, which):
+    """The others are not: the rows that see it have its keys alone, NaN where the scores of these are -inf, and zeros where they see none; parts that begin inside a block too."""
+    b = Batch([(3 * bt + 5, 3), (2 * bt + 70, 90), (2 * bt - 2, 5), (5000, 1)], 4, 2, 64, bt, dtype, seed=bt + which)
+    b.q = b.q.abs() + 0.1
+    keep = []
+    for s, (n, r) in enumerate(zip(b.lens, b.rows)):
+        have = -(-(n + r) // bt)
+        i = which % have
+        only = int(b.table[s, i])
+        b.table[s, :] = -1
+        b.table[s, i] = only
+        b.keys[only, 0, :, 3] = -math.inf
+        keep.append(torch.arange(n + r, device="cuda") // bt == i)
+    out = b.run()
+    assert b.status == 16
+    for s, (n, r) in enumerate(zip(b.lens, b.rows)):
+        seen = (keep[s] & (torch.arange(n + r, device="cuda") <= n + torch.arange(r, device="cuda")[:, None])).any(-1)
+        got = out[b.start[s]:b.start[s + 1]]
+        assert bool((torch.isnan(got[:, :2]) == seen[:, None, None]).all()) and bool((got[~seen] == 0).all())
+        o, e = b.oracle(s, b.hd ** -0.5, keep[s])
+        e = e + (U16 * (1 + U16) * o.abs() if dtype == BF16 else 0)
+        assert bool(((got.double() - o).abs() <= e)[:, 2:].all())
