@@ -837,7 +837,7 @@ __device__ __forceinline__ void paged_tiles(const PagedAttnArgs& a, int id, type
     if (__builtin_expect(has_rows && (__any(odd || ls < PA_FAINT) || a.scale2 == 0.f), 0)) {
       __builtin_amdgcn_s_waitcnt(0x0070);
       const PagedAttnArgs b = args_again();
-      if (!any_block(b, w)) return;
+      if (!any_block(b, w)) continue;
       const unsigned long long again = __ballot(pr < w.n_packed && ((odd ? has_hidden(w, G, pr) : ls < PA_FAINT && has_keys(w, G, pr)) ||
                                                                     (b.scale2 == 0.f && odd_query<BF16, HD>(b, w, kvh, G, pr))));
       for (uint32_t rows = (uint32_t)(again | again >> 32); rows; rows &= rows - 1) redo_row<BF16, HD>(b, w, kvh, G, w0 + 32 * x + __builtin_ctz(rows));

@@ -470,3 +470,16 @@ def test_one_block_of_a_sequence_is_there(dtype, bt, which):
         o, e = b.oracle(s, b.hd ** -0.5, keep[s])
         e = e + (U16 * (1 + U16) * o.abs() if dtype == BF16 else 0)
         assert bool(((got.double() - o).abs() <= e)[:, 2:].all())
+
+
+@pytest.mark.parametrize("case", [c for c in SMALLEST if c[1][5]], ids=name)
+def test_kernel_without_the_prefix(case):
+    """No block of the prefix is in the pool, and the workspace holds NaN: every row has its own keys alone."""
+    import paper_2505_15380_amd as ssd
+    b = Planned(case)
+    b.prefix = [b.keys.shape[0] + i for i in range(b.sb)]
+    keep = [torch.arange(n + r, device="cuda") >= (b.sb * b.bt if j else 0) for n, r, j in zip(b.lens, b.rows, b.joins)]
+    need = ssd.paged_attention_workspace(ssd.Pages(b.keys, b.values), b.nq, len(b.rows), b.n, b.max_len, b.sb)
+    out = b.run(ws=torch.full((need,), 255, dtype=torch.uint8, device="cuda"))
+    assert b.status == 16
+    b.check(out, keep=keep)
